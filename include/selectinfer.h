@@ -38,8 +38,9 @@ extern "C" {
 #endif
 
 /* element types: float32, bfloat16, IEEE half (the paper's float16 storage, Memory Footprint
-   section) */
-typedef enum { SI_F32 = 0, SI_BF16 = 1, SI_F16 = 2 } si_dtype;
+   section); and 8-bit codes (OCP e4m3, no infinities) whose values are code * the scale of their
+   block, for the weights of si_moe_ffn and si_moe_layer alone */
+typedef enum { SI_F32 = 0, SI_BF16 = 1, SI_F16 = 2, SI_E4M3 = 3 } si_dtype;
 
 typedef enum {
     SI_OK = 0,
@@ -412,6 +413,135 @@ int si_load_selected(const void* w_gate, const void* w_up, const void* w_down, i
                      int64_t d, si_dtype wdt, const int32_t* loaded, int64_t L,
                      void* gate_up_c, void* down_c, int32_t* slot_to_orig, int32_t* orig_to_slot,
                      void* hip_stream);
+
+/*
+ * Block-scaled 8-bit matrices (no part of the paper's method: 8-bit weights and activations for
+ * the dense products around selective layers, and for experts).
+ *
+ * si_quantize_fp8: G row-major matrices [R][C] -> codes (OCP e4m3) and one float32 scale for
+ * each block of block_rows x 128 values; blocks are cut at a matrix's edges and do not cross
+ * matrices.
+ *
+ *   x      [G][R][C]  SI_F32, SI_BF16 or SI_F16
+ *   codes  [G][R][C]  uint8 out
+ *   scales [G][ceil(R / block_rows)][ceil(C / 128)]  float32 out
+ *   block_rows        1 (activations) or 128 (weights)
+ *
+ *   a = max(max |x| of the block, 2^-60),  scale = a / 448,  code = e4m3(x * (448 / a))
+ *
+ * in float32, codes rounded to nearest even. A block that holds a NaN or an infinity gets scale
+ * NaN and NaN codes. Requires G, R >= 0, C >= 1, C % 16 == 0, 16-byte aligned x and codes, a
+ * number of blocks below 2^31. G * R = 0 enqueues nothing. Asynchronous, stream-ordered.
+ */
+int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C, int block_rows,
+                    uint8_t* codes, float* scales, void* hip_stream);
+
+/*
+ * Product of two such matrices, y = X W^T:
+ *
+ *   y[m][n] = sum over blocks b of x_scales[m][b] * w_scales[n / 128][b] *
+ *             sum over k in block b of x[m][k] * w[n][k]
+ *
+ *   x [M][K] codes, x_scales [M][ceil(K / 128)]                   (block_rows = 1)
+ *   w [N][K] codes, w_scales [ceil(N / 128)][ceil(K / 128)]       (block_rows = 128)
+ *   y [M][N] out, ydt SI_F32, SI_BF16 or SI_F16, rounded once (to nearest even)
+ *   ws       workspace of si_matmul_fp8_workspace(M, N, K) bytes (NULL when that is 0)
+ *
+ * Accumulation is float32. A NaN code or scale makes the outputs it enters NaN. Requires M >= 0,
+ * N, K >= 1, K % 16 == 0, K <= 2^20, M, N <= 2^24, 16-byte aligned x, w, y and ws. M = 0 enqueues
+ * nothing. Asynchronous, stream-ordered.
+ */
+size_t si_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K);
+int si_matmul_fp8(const uint8_t* x, const float* x_scales, int64_t M, int64_t K, const uint8_t* w,
+                  const float* w_scales, int64_t N, void* y, si_dtype ydt, void* ws,
+                  size_t ws_bytes, void* hip_stream);
+
+/* How si_moe_route scores experts; exactly one of the first two, optionally with the third. */
+enum {
+    SI_ROUTE_SOFTMAX = 1, /* p = softmax of a token's logits over all experts               */
+    SI_ROUTE_SIGMOID = 2, /* p = sigmoid of each logit                                       */
+    SI_ROUTE_RENORM = 4   /* a token's weights are divided by the sum of its chosen p        */
+};
+
+/*
+ * Router of a mixture-of-experts layer (the choice per token of whole experts, beside the
+ * paper's choice of neurons):
+ *
+ *   z[t][e] = w_router[e] . x[t];  p = the scores by mode;  key = z, or p + bias with a bias;
+ *   ids[t]  = the k experts with the largest keys, by decreasing key; equal keys to the lower
+ *             expert, -0 = +0, NaN after every number
+ *   weights[t][r] = scale * p[ids[t][r]], divided by the sum of the chosen p with
+ *             SI_ROUTE_RENORM (0 where that sum is 0)
+ *
+ *   x        [T][d]  SI_F32, SI_BF16 or SI_F16;  w_router [E][d] of x's type or SI_F32
+ *   bias     [E]     float32, optional (NULL): enters the choice, not the weights
+ *   n_valid  (optional, DEVICE int32) tokens t >= *n_valid get ids -1 and weights 0: the rows
+ *            behind the last sequence of a padded batch
+ *   ids      [T][k]  int32 out;  weights [T][k] float32 out
+ *   ws       workspace of si_moe_route_workspace(T, E, d) bytes
+ *
+ * Logits are sums of float32 MFMA results over at most 32 products each, added in float64;
+ * scores, keys and weights are float64, the weights rounded once. A NaN logit makes all softmax
+ * scores of its token NaN. Requires T >= 0, T <= 65535, 1 <= E <= 1024, 1 <= k <= min(E, 32),
+ * d <= 65536, d % 8 == 0 (16-bit x) or d % 4 == 0 (float32 x), 16-byte aligned x, w_router and
+ * ws. Asynchronous, stream-ordered, deterministic.
+ */
+size_t si_moe_route_workspace(int64_t T, int64_t E, int64_t d);
+int si_moe_route(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* w_router,
+                 si_dtype wdt, int64_t E, const float* bias, int64_t k, int mode, float scale,
+                 const int32_t* n_valid, int32_t* ids, float* weights, void* ws, size_t ws_bytes,
+                 void* hip_stream);
+
+/*
+ * The experts of a mixture-of-experts layer, for few tokens:
+ *
+ *   y[t] = sum over r < k of weights[t][r] * W_down[e] (SiLU(W_gate[e] x[t]) * (W_up[e] x[t])),
+ *          e = ids[t][r]
+ *
+ *   x        [T][d]        SI_F32, SI_BF16 or SI_F16
+ *   ids      [T][k]        int32, any order; an id outside [0, E) adds nothing and its weight is
+ *                          not used (a token without any gets y = 0 exactly); an expert listed
+ *                          twice for a token is added twice
+ *   weights  [T][k]        float32
+ *   gate_up  [E][2][I][d]  gate rows, then up rows of each expert; wdt: x's type, or SI_E4M3
+ *                          (x then SI_BF16 or SI_F16)
+ *   down     [E][d][I]     wdt
+ *   gate_up_scales [E][2][ceil(I / 128)][ceil(d / 128)], down_scales [E][ceil(d / 128)][ceil(I /
+ *                          128)]  float32, si_quantize_fp8 with block_rows = 128; NULL unless
+ *                          wdt is SI_E4M3
+ *   y        [T][d] out    ydt: SI_F32 or x's type, rounded once
+ *   ws                     workspace of si_moe_ffn_workspace(...) bytes
+ *
+ * Accumulation is float32; h = SiLU(g) * u is float32 and enters the down product as float32
+ * (float32 weights), as bf16 parts of 16 significant bits in all (24 with a float32 y), or with
+ * half weights as a half pair of 22 bits for |h| < 2^24. Each chosen expert's weights are read
+ * once per 64 of its tokens. Requires 0 <= T <= 512, 1 <= k <= 32, T * k <= 8192, 1 <= E <= 65535; d and I
+ * multiples of 4 (float32), 8 (16-bit) or 16 (SI_E4M3), d, I <= 65536; one expert's gate and up
+ * rows, x as float32, and the parts of h (T * k * I values) each below 2 GiB, else
+ * SI_ERR_UNSUPPORTED; 16-byte aligned x, gate_up, down, y and ws. Asynchronous, stream-ordered,
+ * deterministic.
+ */
+size_t si_moe_ffn_workspace(int64_t T, int64_t k, int64_t E, int64_t d, int64_t I, si_dtype xdt,
+                            si_dtype wdt, si_dtype ydt);
+int si_moe_ffn(const void* x, si_dtype xdt, int64_t T, int64_t d, const int32_t* ids,
+               const float* weights, int64_t k, const void* gate_up, const float* gate_up_scales,
+               const void* down, const float* down_scales, int64_t E, int64_t I, si_dtype wdt,
+               void* y, si_dtype ydt, void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * The whole layer: si_moe_route, then si_moe_ffn with its ids and weights, which are outputs
+ * too. Arguments, limits, results and errors are those of the two calls (rdt: the type of
+ * w_router); y must not overlap ids or weights.
+ *   ws  workspace of si_moe_layer_workspace(...) bytes
+ */
+size_t si_moe_layer_workspace(int64_t T, int64_t k, int64_t E, int64_t d, int64_t I, si_dtype xdt,
+                              si_dtype wdt, si_dtype ydt);
+int si_moe_layer(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* w_router,
+                 si_dtype rdt, const float* bias, int64_t k, int mode, float scale,
+                 const int32_t* n_valid, const void* gate_up, const float* gate_up_scales,
+                 const void* down, const float* down_scales, int64_t E, int64_t I, si_dtype wdt,
+                 int32_t* ids, float* weights, void* y, si_dtype ydt, void* ws, size_t ws_bytes,
+                 void* hip_stream);
 
 #ifdef __cplusplus
 }

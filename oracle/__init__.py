@@ -23,6 +23,15 @@ from .ffn import (  # noqa: F401
     silu,
     stack_step,
 )
+from .experts import (  # noqa: F401
+    decode_e4m3,
+    encode_e4m3,
+    matmul_fp8,
+    moe_ffn,
+    moe_route,
+    quantize_fp8,
+    spread,
+)
 from .selection import (  # noqa: F401
     activations,
     build_loaded_set,

@@ -52,6 +52,20 @@ SIGNATURES = {
     "si_selective_layers": (c_int, [c_i64, c_i64, c_i64, c_vp, c_vp]),
     "si_load_selected": (c_int, [c_vp, c_vp, c_vp, c_i64, c_i64, c_int, c_vp, c_i64, c_vp, c_vp,
                                  c_vp, c_vp, c_vp]),
+    "si_quantize_fp8": (c_int, [c_vp, c_int, c_i64, c_i64, c_i64, c_int, c_vp, c_vp, c_vp]),
+    "si_matmul_fp8_workspace": (c_size, [c_i64, c_i64, c_i64]),
+    "si_matmul_fp8": (c_int, [c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp, c_int, c_vp,
+                              c_size, c_vp]),
+    "si_moe_route_workspace": (c_size, [c_i64, c_i64, c_i64]),
+    "si_moe_route": (c_int, [c_vp, c_int, c_i64, c_i64, c_vp, c_int, c_i64, c_vp, c_i64, c_int,
+                             ctypes.c_float, c_vp, c_vp, c_vp, c_vp, c_size, c_vp]),
+    "si_moe_ffn_workspace": (c_size, [c_i64, c_i64, c_i64, c_i64, c_i64, c_int, c_int, c_int]),
+    "si_moe_ffn": (c_int, [c_vp, c_int, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp, c_vp, c_vp, c_vp,
+                           c_i64, c_i64, c_int, c_vp, c_int, c_vp, c_size, c_vp]),
+    "si_moe_layer_workspace": (c_size, [c_i64, c_i64, c_i64, c_i64, c_i64, c_int, c_int, c_int]),
+    "si_moe_layer": (c_int, [c_vp, c_int, c_i64, c_i64, c_vp, c_int, c_vp, c_i64, c_int,
+                             ctypes.c_float, c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i64, c_int,
+                             c_vp, c_vp, c_vp, c_int, c_vp, c_size, c_vp]),
 }
 
 _lib = None

@@ -13,10 +13,12 @@ import torch
 
 from ._lib import load
 
-F32, BF16, F16 = 0, 1, 2
+F32, BF16, F16, E4M3 = 0, 1, 2, 3
 TOPK_ABS, TOPK_RAW = 1, 2
 FLAG_CHECK, FLAG_SORTED, FLAG_PER_TOKEN, FLAG_FAST_H, FLAG_UNION = 4, 8, 16, 32, 64
 FLAG_EXACT_H = 128
+ROUTE_SOFTMAX, ROUTE_SIGMOID, ROUTE_RENORM = 1, 2, 4
+_SCORES = {"softmax": ROUTE_SOFTMAX, "sigmoid": ROUTE_SIGMOID}
 _MODES = {"abs": TOPK_ABS, "raw": TOPK_RAW}
 
 _DT = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
@@ -464,3 +466,231 @@ def load_selected(w_gate, w_up, w_down, loaded, device=None) -> CompactLayer:
                                  _stream(dev))
     _check(st, "si_load_selected")
     return CompactLayer(gu, dc, s2o, o2s)
+
+
+# ---- block-scaled 8-bit matrices ------------------------------------------------------------
+
+QUANT_BLOCK = 128
+_CODES = (torch.float8_e4m3fn, torch.uint8)
+
+
+def _blocks(n: int) -> int:
+    return -(-n // QUANT_BLOCK)
+
+
+def _need(t, name: str, dev: torch.device, dtype, shape) -> None:
+    """t is a contiguous tensor of that type and shape on that device."""
+    if t.device != dev:
+        raise ValueError(f"{name} must be on {dev}")
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _space(workspace, nbytes: int, dev: torch.device) -> torch.Tensor:
+    """The caller's workspace, or one of this call's own: torch's allocator orders its reuse on
+    the current stream, and a captured graph keeps it, so calls on several streams or in several
+    graphs share nothing."""
+    if workspace is None:
+        return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
+    if workspace.device != dev or not workspace.is_contiguous():
+        raise ValueError(f"workspace must be contiguous and on {dev}")
+    return workspace
+
+
+class _on:
+    """Makes a device current for a call that launches kernels on it."""
+
+    def __init__(self, dev: torch.device):
+        self._guard = None
+        if dev.index is not None and dev.index != torch.cuda.current_device():
+            self._guard = torch.cuda.device(dev)
+
+    def __enter__(self):
+        if self._guard is not None:
+            self._guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self._guard is not None:
+            self._guard.__exit__(*exc)
+
+
+def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | None = None,
+                 scales: torch.Tensor | None = None):
+    """si_quantize_fp8: x [..., R, C] -> (codes float8_e4m3fn [..., R, C], scales float32
+    [..., ceil(R / block_rows), ceil(C / 128)]). block_rows 1 suits activations, 128 weights;
+    leading dimensions are separate matrices. C must be a multiple of 16."""
+    dev = _dev(x)
+    if x.dim() < 2:
+        raise ValueError("x must be [..., R, C]")
+    if block_rows not in (1, QUANT_BLOCK):
+        raise ValueError("block_rows must be 1 or 128")
+    *lead, R, C = x.shape
+    G = 1
+    for n in lead:
+        G *= n
+    sshape = (*lead, R if block_rows == 1 else _blocks(R), _blocks(C))
+    if codes is None:
+        codes = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=dev)
+    if scales is None:
+        scales = torch.empty(sshape, dtype=torch.float32, device=dev)
+    _need(codes, "codes", dev, _CODES, x.shape)
+    _need(scales, "scales", dev, torch.float32, sshape)
+    with _on(dev):
+        st = load().si_quantize_fp8(_ptr(x), _dt(x), G, R, C, block_rows, _ptr(codes),
+                                    _ptr(scales), _stream(dev))
+    _check(st, "si_quantize_fp8")
+    return codes, scales
+
+
+def matmul_fp8(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor,
+               out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
+               workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """si_matmul_fp8: x [M][K] with x_scales [M][ceil(K / 128)] (quantize_fp8 by rows) times w
+    [N][K] with w_scales [ceil(N / 128)][ceil(K / 128)] (by 128 x 128 blocks), y = x w^T
+    [M][N]."""
+    dev = _dev(x)
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        raise ValueError("x must be [M][K] and w [N][K]")
+    (M, K), N = x.shape, w.shape[0]
+    _need(x, "x", dev, _CODES, (M, K))
+    _need(w, "w", dev, _CODES, (N, K))
+    _need(x_scales, "x_scales", dev, torch.float32, (M, _blocks(K)))
+    _need(w_scales, "w_scales", dev, torch.float32, (_blocks(N), _blocks(K)))
+    if out is None:
+        out = torch.empty((M, N), dtype=out_dtype, device=dev)
+    _need(out, "out", dev, out_dtype, (M, N))
+    lib = load()
+    need = lib.si_matmul_fp8_workspace(M, N, K)
+    ws = _space(workspace, need, dev) if need else None
+    with _on(dev):
+        st = lib.si_matmul_fp8(_ptr(x), _ptr(x_scales), M, K, _ptr(w), _ptr(w_scales), N,
+                               _ptr(out), _dt(out), _ptr(ws), ws.numel() if need else 0,
+                               _stream(dev))
+    _check(st, "si_matmul_fp8")
+    return out
+
+
+# ---- mixture of experts ---------------------------------------------------------------------
+
+def _route_args(x, w_router, k, bias, score, renorm, n_valid, ids, weights):
+    """Checked arguments of the router: device, sizes, mode and the two outputs."""
+    dev = _dev(x)
+    if x.dim() != 2 or w_router.dim() != 2:
+        raise ValueError("x must be [T][d] and w_router [E][d]")
+    T, d = x.shape
+    E = w_router.shape[0]
+    _need(x, "x", dev, tuple(_DT), (T, d))
+    _need(w_router, "w_router", dev, (x.dtype, torch.float32), (E, d))
+    if bias is not None:
+        _need(bias, "bias", dev, torch.float32, (E,))
+    if n_valid is not None:
+        if n_valid.device != dev or n_valid.dtype != torch.int32 or n_valid.numel() != 1:
+            raise ValueError("n_valid must be one int32 on x's device")
+    mode = _SCORES[score] | (ROUTE_RENORM if renorm else 0)
+    if k < 0:
+        raise ValueError("k must not be negative")
+    if ids is None:
+        ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+    if weights is None:
+        weights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    _need(ids, "ids", dev, torch.int32, (T, k))
+    _need(weights, "weights", dev, torch.float32, (T, k))
+    return dev, T, d, E, mode, ids, weights
+
+
+def _expert_args(x, gate_up, down, gate_up_scales, down_scales, out_dtype, y):
+    """Checked expert weights: I, their type code, and y."""
+    dev, (T, d) = x.device, x.shape
+    if gate_up.dim() != 4:
+        raise ValueError("gate_up must be [E][2][I][d]")
+    E, _, inter, _ = gate_up.shape
+    fp8 = gate_up.dtype in _CODES
+    kind = _CODES if fp8 else (x.dtype,)
+    _need(gate_up, "gate_up", dev, kind, (E, 2, inter, d))
+    _need(down, "down", dev, kind, (E, d, inter))
+    if fp8 != (gate_up_scales is not None) or fp8 != (down_scales is not None):
+        raise ValueError("8-bit experts need gate_up_scales and down_scales, others take none")
+    if fp8:
+        _need(gate_up_scales, "gate_up_scales", dev, torch.float32,
+              (E, 2, _blocks(inter), _blocks(d)))
+        _need(down_scales, "down_scales", dev, torch.float32, (E, _blocks(d), _blocks(inter)))
+    if y is None:
+        y = torch.empty((T, d), dtype=out_dtype or torch.float32, device=dev)
+    _need(y, "y", dev, out_dtype or (torch.float32, x.dtype), (T, d))
+    return E, inter, E4M3 if fp8 else _dt(x), y
+
+
+def moe_route(x: torch.Tensor, w_router: torch.Tensor, k: int, bias: torch.Tensor | None = None,
+              score: str = "softmax", renorm: bool = True, scale: float = 1.0,
+              n_valid: torch.Tensor | None = None, ids: torch.Tensor | None = None,
+              weights: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """si_moe_route: the k experts of each token by their router scores -> (ids [T][k] int32 by
+    decreasing score, weights [T][k] float32). score "softmax" or "sigmoid"; bias [E] enters the
+    choice only; renorm divides by the chosen scores' sum; tokens from n_valid (one int32 on the
+    device) on get ids -1 and weights 0."""
+    dev, T, d, E, mode, ids, weights = _route_args(x, w_router, k, bias, score, renorm, n_valid,
+                                                   ids, weights)
+    lib = load()
+    ws = _space(workspace, lib.si_moe_route_workspace(T, E, d), dev)
+    with _on(dev):
+        st = lib.si_moe_route(_ptr(x), _dt(x), T, d, _ptr(w_router), _dt(w_router), E, _ptr(bias),
+                              k, mode, float(scale), _ptr(n_valid), _ptr(ids), _ptr(weights),
+                              _ptr(ws), ws.numel(), _stream(dev))
+    _check(st, "si_moe_route")
+    return ids, weights
+
+
+def moe_ffn(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate_up: torch.Tensor,
+            down: torch.Tensor, gate_up_scales: torch.Tensor | None = None,
+            down_scales: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+            y: torch.Tensor | None = None, workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """si_moe_ffn: the experts ids [T][k] of each token of x [T][d], weighted by weights [T][k]
+    float32 -> y [T][d] (float32, or x's type with out_dtype). gate_up [E][2][I][d] and down
+    [E][d][I] of x's type, or e4m3 codes with their 128 x 128 block scales (quantize_fp8 with
+    block_rows=128). Ids outside [0, E) add nothing. At most 512 tokens."""
+    dev = _dev(x)
+    if x.dim() != 2 or ids.dim() != 2:
+        raise ValueError("x must be [T][d] and ids [T][k]")
+    (T, d), k = x.shape, ids.shape[1]
+    _need(x, "x", dev, tuple(_DT), (T, d))
+    _need(ids, "ids", dev, torch.int32, (T, k))
+    _need(weights, "weights", dev, torch.float32, (T, k))
+    E, inter, wdt, y = _expert_args(x, gate_up, down, gate_up_scales, down_scales, out_dtype, y)
+    lib, xdt, ydt = load(), _dt(x), _dt(y)
+    ws = _space(workspace, lib.si_moe_ffn_workspace(T, k, E, d, inter, xdt, wdt, ydt), dev)
+    with _on(dev):
+        st = lib.si_moe_ffn(_ptr(x), xdt, T, d, _ptr(ids), _ptr(weights), k, _ptr(gate_up),
+                            _ptr(gate_up_scales), _ptr(down), _ptr(down_scales), E, inter, wdt,
+                            _ptr(y), ydt, _ptr(ws), ws.numel(), _stream(dev))
+    _check(st, "si_moe_ffn")
+    return y
+
+
+def moe_layer(x: torch.Tensor, w_router: torch.Tensor, gate_up: torch.Tensor, down: torch.Tensor,
+              k: int, bias: torch.Tensor | None = None, score: str = "softmax",
+              renorm: bool = True, scale: float = 1.0, n_valid: torch.Tensor | None = None,
+              gate_up_scales: torch.Tensor | None = None,
+              down_scales: torch.Tensor | None = None, out_dtype: torch.dtype | None = None,
+              y: torch.Tensor | None = None, ids: torch.Tensor | None = None,
+              weights: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """si_moe_layer: moe_route, then moe_ffn with its choice, in one call -> (y, ids, weights).
+    Arguments as for the two."""
+    dev, T, d, E, mode, ids, weights = _route_args(x, w_router, k, bias, score, renorm, n_valid,
+                                                   ids, weights)
+    En, inter, wdt, y = _expert_args(x, gate_up, down, gate_up_scales, down_scales, out_dtype, y)
+    if En != E:
+        raise ValueError("w_router and gate_up must have one number of experts")
+    lib, xdt, ydt = load(), _dt(x), _dt(y)
+    ws = _space(workspace, lib.si_moe_layer_workspace(T, k, E, d, inter, xdt, wdt, ydt), dev)
+    with _on(dev):
+        st = lib.si_moe_layer(_ptr(x), xdt, T, d, _ptr(w_router), _dt(w_router), _ptr(bias), k,
+                              mode, float(scale), _ptr(n_valid), _ptr(gate_up),
+                              _ptr(gate_up_scales), _ptr(down), _ptr(down_scales), E, inter, wdt,
+                              _ptr(ids), _ptr(weights), _ptr(y), ydt, _ptr(ws), ws.numel(),
+                              _stream(dev))
+    _check(st, "si_moe_layer")
+    return y, ids, weights

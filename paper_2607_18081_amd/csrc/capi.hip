@@ -168,6 +168,54 @@ int selective_ffn(const void* x, si_dtype xdt, int64_t B, int64_t d, const int32
                                       rn));
 }
 
+// ---- 8-bit matrices and experts: argument checks --------------------------------------------
+
+constexpr int64_t kMaxDim = 65536, kMaxTokens = 512, kMaxPicks = 32, kMaxPairs = 8192;
+
+// x's rows hold whole 16-byte vectors
+bool whole_rows(int64_t n, int dt) {
+    return n % (dt == SI_F32 ? 4 : (dt == SI_E4M3 ? 16 : 8)) == 0;
+}
+
+bool valid_route_mode(int mode) {
+    const int score = mode & ~SI_ROUTE_RENORM;
+    return score == SI_ROUTE_SOFTMAX || score == SI_ROUTE_SIGMOID;
+}
+
+// sizes and types of si_moe_route; T may be 0
+int check_route(si_dtype xdt, int64_t T, int64_t d, si_dtype rdt, int64_t E, int64_t k, int mode,
+                float scale) {
+    if (T < 0 || d < 1 || E < 1 || k < 1 || k > E) return SI_ERR_INVALID;
+    if (!valid_route_mode(mode) || !(scale - scale == 0.0f)) return SI_ERR_INVALID;
+    if (!valid_dtype(xdt) || (rdt != xdt && rdt != SI_F32)) return SI_ERR_UNSUPPORTED;
+    if (T > 65535 || E > 1024 || k > kMaxPicks || d > kMaxDim || !whole_rows(d, xdt))
+        return SI_ERR_UNSUPPORTED;
+    return SI_OK;
+}
+
+// sizes and types of si_moe_ffn; T may be 0
+int check_experts(si_dtype xdt, int64_t T, int64_t d, int64_t k, int64_t E, int64_t I,
+                  si_dtype wdt, si_dtype ydt) {
+    if (T < 0 || d < 1 || E < 1 || k < 1 || I < 1) return SI_ERR_INVALID;
+    if (!valid_dtype(xdt) || !(wdt == xdt || (wdt == SI_E4M3 && xdt != SI_F32)))
+        return SI_ERR_UNSUPPORTED;
+    if (ydt != SI_F32 && ydt != xdt) return SI_ERR_UNSUPPORTED;
+    if (T > kMaxTokens || k > kMaxPicks || T * k > kMaxPairs || E > 65535 || d > kMaxDim || I > kMaxDim ||
+        !whole_rows(d, wdt) || !whole_rows(I, wdt) || !si::moe_supported(T, k, d, I, xdt, wdt, ydt))
+        return SI_ERR_UNSUPPORTED;
+    return SI_OK;
+}
+
+// buffers of si_moe_ffn (ids and weights apart)
+bool bad_expert_buffers(const void* x, const void* gate_up, const float* gus, const void* down,
+                        const float* dns, si_dtype wdt, const void* y) {
+    if (!x || !gate_up || !down || !y) return true;
+    if (wdt == SI_E4M3 && (!gus || !dns)) return true;
+    return !aligned16(x) || !aligned16(gate_up) || !aligned16(down) || !aligned16(y);
+}
+
+size_t round256(size_t n) { return (n + 255) / 256 * 256; }
+
 }  // namespace
 
 extern "C" {
@@ -428,6 +476,116 @@ int si_merge_scores(const double* scores, const int64_t* tokens, int64_t F, int6
 int si_rank_neurons(const double* scores, int64_t N, int32_t* order, void* hip_stream) {
     if (N < 1 || N > (1 << 24) || !scores || !order) return SI_ERR_INVALID;
     return from_hip(si::launch_rank(scores, N, order, static_cast<hipStream_t>(hip_stream)));
+}
+
+int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C, int block_rows,
+                    uint8_t* codes, float* scales, void* hip_stream) {
+    if (G < 0 || R < 0 || C < 1 || (block_rows != 1 && block_rows != 128)) return SI_ERR_INVALID;
+    if (!valid_dtype(xdt)) return SI_ERR_UNSUPPORTED;
+    if (C % 16 != 0) return SI_ERR_UNSUPPORTED;
+    if (G == 0 || R == 0) return SI_OK;
+    // no product below leaves 64 bits
+    constexpr int64_t top = (int64_t)1 << 31;
+    if (G > top || R > top || C > top || G > ((int64_t)1 << 40) / R ||
+        si::quant_groups(G, R, C, block_rows) >= top)
+        return SI_ERR_UNSUPPORTED;
+    if (!x || !codes || !scales || !aligned16(x) || !aligned16(codes)) return SI_ERR_INVALID;
+    return from_hip(si::launch_quant(x, xdt, G, R, C, block_rows, codes, scales,
+                                     static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t si_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K) {
+    if (M < 1 || N < 1 || K < 1) return 0;
+    return si::fp8_workspace(M, N, K);
+}
+
+int si_matmul_fp8(const uint8_t* x, const float* x_scales, int64_t M, int64_t K, const uint8_t* w,
+                  const float* w_scales, int64_t N, void* y, si_dtype ydt, void* ws,
+                  size_t ws_bytes, void* hip_stream) {
+    if (M < 0 || N < 1 || K < 1) return SI_ERR_INVALID;
+    if (!valid_dtype(ydt)) return SI_ERR_UNSUPPORTED;
+    if (K % 16 != 0 || K > (1 << 20) || M > (1 << 24) || N > (1 << 24)) return SI_ERR_UNSUPPORTED;
+    if (M == 0) return SI_OK;
+    if (!x || !x_scales || !w || !w_scales || !y) return SI_ERR_INVALID;
+    if (!aligned16(x) || !aligned16(w) || !aligned16(y)) return SI_ERR_INVALID;
+    const size_t need = si_matmul_fp8_workspace(M, N, K);
+    if (need > 0 && (!ws || ws_bytes < need || !aligned16(ws))) return SI_ERR_WORKSPACE;
+    return from_hip(si::launch_matmul_fp8(x, x_scales, M, K, w, w_scales, N, y, ydt, ws,
+                                          static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t si_moe_route_workspace(int64_t T, int64_t E, int64_t d) {
+    if (T < 1 || E < 1 || d < 1) return 0;
+    return si::route_workspace(T, E, d);
+}
+
+int si_moe_route(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* w_router,
+                 si_dtype wdt, int64_t E, const float* bias, int64_t k, int mode, float scale,
+                 const int32_t* n_valid, int32_t* ids, float* weights, void* ws, size_t ws_bytes,
+                 void* hip_stream) {
+    const int bad = check_route(xdt, T, d, wdt, E, k, mode, scale);
+    if (bad) return bad;
+    if (T == 0) return SI_OK;
+    if (!x || !w_router || !ids || !weights || !aligned16(x) || !aligned16(w_router))
+        return SI_ERR_INVALID;
+    if (!ws || ws_bytes < si_moe_route_workspace(T, E, d) || !aligned16(ws))
+        return SI_ERR_WORKSPACE;
+    return from_hip(si::launch_route(x, xdt, T, d, w_router, wdt, E, bias, k,
+                                     (mode & SI_ROUTE_SIGMOID) != 0, (mode & SI_ROUTE_RENORM) != 0,
+                                     scale, n_valid, ids, weights, ws,
+                                     static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t si_moe_ffn_workspace(int64_t T, int64_t k, int64_t E, int64_t d, int64_t I, si_dtype xdt,
+                            si_dtype wdt, si_dtype ydt) {
+    if (T < 1 || check_experts(xdt, T, d, k, E, I, wdt, ydt) != SI_OK) return 0;
+    return si::moe_workspace(T, k, d, I, xdt, wdt, ydt);
+}
+
+int si_moe_ffn(const void* x, si_dtype xdt, int64_t T, int64_t d, const int32_t* ids,
+               const float* weights, int64_t k, const void* gate_up, const float* gate_up_scales,
+               const void* down, const float* down_scales, int64_t E, int64_t I, si_dtype wdt,
+               void* y, si_dtype ydt, void* ws, size_t ws_bytes, void* hip_stream) {
+    const int bad = check_experts(xdt, T, d, k, E, I, wdt, ydt);
+    if (bad) return bad;
+    if (T == 0) return SI_OK;
+    if (!ids || !weights) return SI_ERR_INVALID;
+    if (bad_expert_buffers(x, gate_up, gate_up_scales, down, down_scales, wdt, y))
+        return SI_ERR_INVALID;
+    if (!ws || ws_bytes < si_moe_ffn_workspace(T, k, E, d, I, xdt, wdt, ydt) || !aligned16(ws))
+        return SI_ERR_WORKSPACE;
+    return from_hip(si::launch_moe(x, xdt, T, d, ids, weights, k, gate_up, gate_up_scales, down,
+                                   down_scales, E, I, wdt, y, ydt, ws,
+                                   static_cast<hipStream_t>(hip_stream)));
+}
+
+size_t si_moe_layer_workspace(int64_t T, int64_t k, int64_t E, int64_t d, int64_t I, si_dtype xdt,
+                              si_dtype wdt, si_dtype ydt) {
+    const size_t ffn = si_moe_ffn_workspace(T, k, E, d, I, xdt, wdt, ydt);
+    return ffn ? round256(ffn) + si_moe_route_workspace(T, E, d) : 0;
+}
+
+int si_moe_layer(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* w_router,
+                 si_dtype rdt, const float* bias, int64_t k, int mode, float scale,
+                 const int32_t* n_valid, const void* gate_up, const float* gate_up_scales,
+                 const void* down, const float* down_scales, int64_t E, int64_t I, si_dtype wdt,
+                 int32_t* ids, float* weights, void* y, si_dtype ydt, void* ws, size_t ws_bytes,
+                 void* hip_stream) {
+    int bad = check_route(xdt, T, d, rdt, E, k, mode, scale);
+    if (!bad) bad = check_experts(xdt, T, d, k, E, I, wdt, ydt);
+    if (bad) return bad;
+    if (T == 0) return SI_OK;
+    if (!w_router || !ids || !weights || !aligned16(w_router)) return SI_ERR_INVALID;
+    if (bad_expert_buffers(x, gate_up, gate_up_scales, down, down_scales, wdt, y))
+        return SI_ERR_INVALID;
+    const size_t ffn = round256(si_moe_ffn_workspace(T, k, E, d, I, xdt, wdt, ydt));
+    if (!ws || ws_bytes < si_moe_layer_workspace(T, k, E, d, I, xdt, wdt, ydt) || !aligned16(ws))
+        return SI_ERR_WORKSPACE;
+    bad = si_moe_route(x, xdt, T, d, w_router, rdt, E, bias, k, mode, scale, n_valid, ids, weights,
+                       static_cast<char*>(ws) + ffn, ws_bytes - ffn, hip_stream);
+    if (bad) return bad;
+    return si_moe_ffn(x, xdt, T, d, ids, weights, k, gate_up, gate_up_scales, down, down_scales, E,
+                      I, wdt, y, ydt, ws, ffn, hip_stream);
 }
 
 }  // extern "C"

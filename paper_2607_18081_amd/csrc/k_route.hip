@@ -1,0 +1,248 @@
+// The router of a mixture-of-experts layer: logits z = W x, the k experts of each token, and
+// their weights.
+//
+//   score p = softmax(z) over the experts, or sigmoid(z)
+//   key     = z, or p + bias where a choice bias is given
+//   chosen  : the k largest keys, equal keys to the lower expert, NaN after every number
+//   weight  = scale * p / (sum of the chosen p, in rank order)   (or scale * p)
+//
+// Which experts a token takes is a comparison of sums, so the sums are kept from depending on
+// their order as far as it costs nothing: MFMAs of 16-bit data add 32 products in float32, and
+// those short sums are added in float64, as are the parts of a split reduction. Scores, keys and
+// weights are float64 too (E of them a token) and the weights are rounded once.
+#include "common.h"
+#include "launch.h"
+#include "mfma.h"
+
+namespace si {
+
+namespace {
+
+// ---- logits ------------------------------------------------------------------------------
+// One work-group of 4 waves a tile of 16 experts x 16 tokens and a K chunk; the waves take K
+// steps in turn. The experts' rows are the MFMA's M operand, tokens its N operand.
+
+// operands of one K step: 16 bytes of a weight row a lane (four lanes a row: 32 values of 16-bit
+// data, 16 of float32), and the same columns of a token
+template <typename XT, typename WT>
+struct Step;
+template <typename T>
+struct Step<T, T> {
+    static constexpr int K = 4 * Elem<T>::V;
+    __device__ __forceinline__ static f32x4_t mma(__amdgpu_buffer_rsrc_t w, int wo,
+                                                  __amdgpu_buffer_rsrc_t x, int xo) {
+        const f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+        return Mfma<T>::mma(Mfma<T>::vec(bload16(w, wo)), Mfma<T>::vec(bload16(x, xo)), z);
+    }
+};
+__device__ __forceinline__ f32x4_t mma_f32(const V16& a, const float* b) {
+    f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w[e]), b[e], z, 0, 0, 0);
+    return z;
+}
+template <>
+struct Step<float, float> {
+    static constexpr int K = 16;
+    __device__ __forceinline__ static f32x4_t mma(__amdgpu_buffer_rsrc_t w, int wo,
+                                                  __amdgpu_buffer_rsrc_t x, int xo) {
+        float f[4];
+        Elem<float>::unpack(bload16(x, xo), f);
+        return mma_f32(bload16(w, wo), f);
+    }
+};
+// a float32 router over 16-bit activations
+template <typename XT>
+struct Step<XT, float> {
+    static constexpr int K = 16;
+    __device__ __forceinline__ static f32x4_t mma(__amdgpu_buffer_rsrc_t w, int wo,
+                                                  __amdgpu_buffer_rsrc_t x, int xo) {
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(x, xo, 0, 0);
+        V16 t{{(uint32_t)v[0], (uint32_t)v[1], 0u, 0u}};
+        float f[8];
+        Elem<XT>::unpack(t, f);
+        return mma_f32(bload16(w, wo), f);
+    }
+};
+
+constexpr int kLogitWaves = 4;
+
+template <typename XT, typename WT>
+__global__ __launch_bounds__(kLogitWaves * 64) void route_logits(
+    const XT* __restrict__ x, const WT* __restrict__ w, int T, int E, int64_t d, int kchunk,
+    double* __restrict__ part) {
+    using S = Step<XT, WT>;
+    __shared__ double red[kLogitWaves][256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int row = lane & 15, g = lane >> 4;
+    const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
+    // rows of the two operand tiles only: 32-bit offsets hold for any number of tokens
+    const auto wr = make_rsrc(w + (int64_t)e0 * d, (int64_t)min(16, E - e0) * d * sizeof(WT));
+    const auto xr = make_rsrc(x + (int64_t)t0 * d, (int64_t)min(16, T - t0) * d * sizeof(XT));
+    const int k0 = blockIdx.z * kchunk, k1 = min((int)d, k0 + kchunk);
+    constexpr int V = S::K / 4;  // values a lane
+    double acc[4] = {0.0, 0.0, 0.0, 0.0};
+    for (int k = k0 + wave * S::K; k < k1; k += kLogitWaves * S::K) {
+        const int c = k + V * g;
+        const bool in = c < k1;
+        const int wo = (in & (e0 + row < E)) ? (int)((row * d + c) * sizeof(WT)) : kOOB;
+        const int xo = (in & (t0 + row < T)) ? (int)((row * d + c) * sizeof(XT)) : kOOB;
+        const f32x4_t s = S::mma(wr, wo, xr, xo);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[i] += (double)s[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) red[wave][row * 16 + 4 * g + i] = acc[i];  // [token][expert]
+    __syncthreads();
+    const int t = threadIdx.x >> 4, e = threadIdx.x & 15;
+    double s = red[0][threadIdx.x];
+#pragma unroll
+    for (int v = 1; v < kLogitWaves; ++v) s += red[v][threadIdx.x];
+    if (t0 + t < T && e0 + e < E)
+        part[((int64_t)blockIdx.z * T + t0 + t) * E + e0 + e] = s;
+}
+
+// ---- choice ------------------------------------------------------------------------------
+
+// order key: unsigned order equals the order of the values, -0 = +0, NaN below every number
+__device__ __forceinline__ uint64_t key_of(double v) {
+    if (!(v == v)) return 1u;
+    v += 0.0;  // -0 -> +0
+    const uint64_t u = (uint64_t)__double_as_longlong(v);
+    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
+}
+
+// Fixed-order sum or maximum over the work-group's values
+template <bool MAX>
+__device__ __forceinline__ double group_reduce(double v, double* red) {
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) {
+        const double o = __shfl_xor(v, m, kWave);
+        v = MAX ? fmax(v, o) : v + o;
+    }
+    const int n = blockDim.x >> 6;
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+    for (int i = 1; i < n; ++i) v = MAX ? fmax(v, red[i]) : v + red[i];
+    return v;
+}
+
+// One work-group of 1024 threads a token. Thread i < EP owns expert i; an expert's rank is the
+// number of experts before it in the order, counted by 1024 / EP threads an expert from the keys
+// in LDS: E * E / 1024 comparisons a thread and one exchange, where k rounds of a maximum over
+// the work-group would take 10 steps of exchange each.
+__global__ __launch_bounds__(1024) void route_choose(
+    const double* __restrict__ part, int KS, int T, int E, int EP, const float* __restrict__ bias,
+    int k, int sigmoid, int renorm, float scale, const int32_t* __restrict__ n_valid,
+    int32_t* __restrict__ ids, float* __restrict__ weights) {
+    __shared__ uint64_t keys[1024];
+    __shared__ int rank[1024];
+    __shared__ double red[16];
+    __shared__ double chosen[64];
+    const int t = blockIdx.x, i = threadIdx.x;
+    if (n_valid && t >= *n_valid) {
+        if (i < k) {
+            ids[(int64_t)t * k + i] = -1;
+            weights[(int64_t)t * k + i] = 0.0f;
+        }
+        return;
+    }
+    const bool mine = i < E;
+    double z = 0.0;
+    if (mine)
+        for (int s = 0; s < KS; ++s) z += part[((int64_t)s * T + t) * E + i];
+    double p;
+    if (sigmoid) {
+        p = 1.0 / (1.0 + exp(-z));
+    } else {
+        const double top = group_reduce<true>(mine ? z : -HUGE_VAL, red);
+        p = mine ? exp(z - top) : 0.0;
+        p /= group_reduce<false>(p, red);
+    }
+    uint64_t key = 0u;  // below every expert's
+    if (mine) key = key_of(bias ? p + (double)bias[i] : z);
+    keys[i] = key;
+    rank[i] = 0;
+    __syncthreads();
+    // thread i counts for expert i % EP over the 1024 / EP-th part of the experts
+    const int me = i & (EP - 1);
+    if (me < E) {
+        const int parts = 1024 / EP, per = (E + parts - 1) / parts;
+        const int lo = min(E, (i / EP) * per), hi = min(E, lo + per);
+        const uint64_t m = keys[me];
+        int n = 0;
+        for (int j = lo; j < hi; ++j) n += keys[j] > m - (uint64_t)(j < me);
+        if (n) atomicAdd(&rank[me], n);  // whole numbers: the order of the additions is free
+    }
+    __syncthreads();
+    const int r = mine ? rank[i] : k;
+    if (r < k) {
+        chosen[r] = p;
+        ids[(int64_t)t * k + r] = i;
+    }
+    __syncthreads();
+    if (r < k) {
+        double w = p;
+        if (renorm) {
+            double sum = 0.0;
+            for (int j = 0; j < k; ++j) sum += chosen[j];
+            w = sum > 0.0 || !(sum == sum) ? p / sum : 0.0;
+        }
+        weights[(int64_t)t * k + r] = (float)(w * (double)scale);
+    }
+}
+
+template <typename XT, typename WT>
+void logits(const void* x, const void* w, int64_t T, int64_t E, int64_t d, int kchunk, int KS,
+            double* part, hipStream_t s) {
+    const dim3 grid((unsigned)((E + 15) / 16), (unsigned)((T + 15) / 16), (unsigned)KS);
+    route_logits<XT, WT><<<grid, kLogitWaves * 64, 0, s>>>(
+        static_cast<const XT*>(x), static_cast<const WT*>(w), (int)T, (int)E, d, kchunk, part);
+}
+
+}  // namespace
+
+// K chunks of the logits: enough work-groups to spread a small call over the chip (512 columns
+// each at least), one chunk where the tiles of experts and tokens do that alone
+int route_chunks(int64_t T, int64_t E, int64_t d) {
+    const int64_t tiles = ((E + 15) / 16) * ((T + 15) / 16);
+    int64_t ks = (1024 + tiles - 1) / tiles;
+    const int64_t most = (d + 511) / 512;
+    if (ks > most) ks = most;
+    if (ks > 16) ks = 16;
+    return (int)ks;
+}
+
+size_t route_workspace(int64_t T, int64_t E, int64_t d) {
+    return (size_t)route_chunks(T, E, d) * T * E * sizeof(double);
+}
+
+hipError_t launch_route(const void* x, int xdt, int64_t T, int64_t d, const void* w, int wdt,
+                        int64_t E, const float* bias, int64_t k, int sigmoid, int renorm,
+                        float scale, const int32_t* n_valid, int32_t* ids, float* weights,
+                        void* ws, hipStream_t s) {
+    const int KS = route_chunks(T, E, d);
+    // chunks of whole 32-value steps
+    const int kchunk = (int)(((d + KS - 1) / KS + 31) / 32 * 32);
+    double* part = static_cast<double*>(ws);
+    if (xdt == 0)
+        logits<float, float>(x, w, T, E, d, kchunk, KS, part, s);
+    else if (xdt == 1 && wdt == 1)
+        logits<bf16_t, bf16_t>(x, w, T, E, d, kchunk, KS, part, s);
+    else if (xdt == 1)
+        logits<bf16_t, float>(x, w, T, E, d, kchunk, KS, part, s);
+    else if (wdt == 2)
+        logits<f16_t, f16_t>(x, w, T, E, d, kchunk, KS, part, s);
+    else
+        logits<f16_t, float>(x, w, T, E, d, kchunk, KS, part, s);
+    int EP = 64;
+    while (EP < E) EP *= 2;
+    route_choose<<<dim3((unsigned)T), 1024, 0, s>>>(part, KS, (int)T, (int)E, EP, bias, (int)k,
+                                                   sigmoid, renorm, scale, n_valid, ids, weights);
+    return hipGetLastError();
+}
+
+}  // namespace si

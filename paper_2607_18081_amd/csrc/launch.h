@@ -150,4 +150,27 @@ hipError_t launch_check_csr(const int32_t* offsets, const int32_t* idx, int64_t 
 hipError_t launch_residual_rmsnorm(const void* x, int xdt, const float* y, int64_t B, int64_t d,
                                    float eps, void* x_out, hipStream_t s);
 
+// ---- k_quant.hip, k_fp8.hip: block-scaled 8-bit matrices ----------------------------------
+// work-groups of a quantisation (block_rows 1 or 128)
+int64_t quant_groups(int64_t G, int64_t R, int64_t C, int block_rows);
+hipError_t launch_quant(const void* x, int xdt, int64_t G, int64_t R, int64_t C, int block_rows,
+                        uint8_t* codes, float* scales, hipStream_t s);
+size_t fp8_workspace(int64_t M, int64_t N, int64_t K);
+hipError_t launch_matmul_fp8(const uint8_t* x, const float* xs, int64_t M, int64_t K,
+                             const uint8_t* w, const float* ws, int64_t N, void* y, int ydt,
+                             void* wsp, hipStream_t s);
+
+// ---- k_route.hip, k_moe.hip: mixture of experts -------------------------------------------
+size_t route_workspace(int64_t T, int64_t E, int64_t d);
+hipError_t launch_route(const void* x, int xdt, int64_t T, int64_t d, const void* w, int wdt,
+                        int64_t E, const float* bias, int64_t k, int sigmoid, int renorm,
+                        float scale, const int32_t* n_valid, int32_t* ids, float* weights,
+                        void* ws, hipStream_t s);
+size_t moe_workspace(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt, int ydt);
+bool moe_supported(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt, int ydt);
+hipError_t launch_moe(const void* x, int xdt, int64_t T, int64_t d, const int32_t* ids,
+                      const float* w, int64_t k, const void* gate_up, const float* gus,
+                      const void* down, const float* dns, int64_t E, int64_t I, int wdt, void* y,
+                      int ydt, void* ws, hipStream_t s);
+
 }  // namespace si
