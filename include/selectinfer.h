@@ -447,11 +447,18 @@ int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C
  *   y [M][N] out, ydt SI_F32, SI_BF16 or SI_F16, rounded once (to nearest even)
  *   ws       workspace of si_matmul_fp8_workspace(M, N, K) bytes (NULL when that is 0)
  *
- * Accumulation is float32. A NaN code or scale makes the outputs it enters NaN. Requires M >= 0,
+ * Blocks are added in float32. The products of a block are summed in float32 for a float32 y; for
+ * a 16-bit y by the 8-bit matrix instruction, which drops what lies 2^-14 below the block's largest
+ * product (a relative error near 1.5e-5, far below the rounding of y). A NaN code or scale makes
+ * the outputs it enters NaN. Requires M >= 0,
  * N, K >= 1, K % 16 == 0, K <= 2^20, M, N <= 2^24, 16-byte aligned x, w, y and ws. M = 0 enqueues
  * nothing. Asynchronous, stream-ordered.
+ *
+ * si_matmul_fp8_plan: plan[0..1], weight rows and tokens of the tile that a call of these sizes
+ * takes (0, 0: 16 rows with all tokens), plan[2], its K chunks (for tests and measurements).
  */
 size_t si_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K);
+int si_matmul_fp8_plan(int64_t M, int64_t N, int64_t K, si_dtype ydt, int32_t* plan);
 int si_matmul_fp8(const uint8_t* x, const float* x_scales, int64_t M, int64_t K, const uint8_t* w,
                   const float* w_scales, int64_t N, void* y, si_dtype ydt, void* ws,
                   size_t ws_bytes, void* hip_stream);

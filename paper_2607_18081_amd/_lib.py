@@ -54,6 +54,7 @@ SIGNATURES = {
                                  c_vp, c_vp, c_vp]),
     "si_quantize_fp8": (c_int, [c_vp, c_int, c_i64, c_i64, c_i64, c_int, c_vp, c_vp, c_vp]),
     "si_matmul_fp8_workspace": (c_size, [c_i64, c_i64, c_i64]),
+    "si_matmul_fp8_plan": (c_int, [c_i64, c_i64, c_i64, c_int, c_vp]),
     "si_matmul_fp8": (c_int, [c_vp, c_vp, c_i64, c_i64, c_vp, c_vp, c_i64, c_vp, c_int, c_vp,
                               c_size, c_vp]),
     "si_moe_route_workspace": (c_size, [c_i64, c_i64, c_i64]),

@@ -546,6 +546,14 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | Non
     return codes, scales
 
 
+def matmul_fp8_plan(M: int, N: int, K: int, out_dtype: torch.dtype = torch.bfloat16) -> tuple:
+    """si_matmul_fp8_plan: (weight rows, tokens of the tile, K chunks) of a product of these sizes;
+    rows 0: 16 rows with all tokens. Needs no GPU."""
+    out = (ctypes.c_int32 * 3)()
+    _check(load().si_matmul_fp8_plan(M, N, K, _DT[out_dtype], out), "si_matmul_fp8_plan")
+    return tuple(out)
+
+
 def matmul_fp8(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_scales: torch.Tensor,
                out_dtype: torch.dtype = torch.bfloat16, out: torch.Tensor | None = None,
                workspace: torch.Tensor | None = None) -> torch.Tensor:

@@ -499,6 +499,13 @@ size_t si_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K) {
     return si::fp8_workspace(M, N, K);
 }
 
+int si_matmul_fp8_plan(int64_t M, int64_t N, int64_t K, si_dtype ydt, int32_t* plan) {
+    if (M < 1 || N < 1 || K < 1 || !plan) return SI_ERR_INVALID;
+    if (!valid_dtype(ydt)) return SI_ERR_UNSUPPORTED;
+    si::fp8_tiles_of(M, N, K, ydt, plan);
+    return SI_OK;
+}
+
 int si_matmul_fp8(const uint8_t* x, const float* x_scales, int64_t M, int64_t K, const uint8_t* w,
                   const float* w_scales, int64_t N, void* y, si_dtype ydt, void* ws,
                   size_t ws_bytes, void* hip_stream) {

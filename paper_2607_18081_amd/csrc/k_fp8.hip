@@ -16,6 +16,7 @@
 #include "common.h"
 #include "launch.h"
 #include "mfma.h"
+#include "pipe.h"
 
 namespace si {
 
@@ -69,101 +70,493 @@ __device__ __forceinline__ void put(bf16_t* y, float v) {
     *y = __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 __device__ __forceinline__ void put(f16_t* y, float v) { *y = (f16_t)v; }
+// eight values at an 8-element aligned place
+__device__ __forceinline__ void put8(float* y, const f32x4_t& a, const f32x4_t& b) {
+    *reinterpret_cast<f32x4_t*>(y) = a;
+    *reinterpret_cast<f32x4_t*>(y + 4) = b;
+}
+template <typename T16>
+__device__ __forceinline__ void put8(T16* y, const f32x4_t& a, const f32x4_t& b) {
+    T16 o[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        put(o + e, a[e]);
+        put(o + 4 + e, b[e]);
+    }
+    V16 u;
+    __builtin_memcpy(&u, o, 16);
+    st16(y, u);
+}
+// four values at a 4-element aligned place
+__device__ __forceinline__ void put4(float* y, const f32x4_t& v) {
+    *reinterpret_cast<f32x4_t*>(y) = v;
+}
+template <typename T16>
+__device__ __forceinline__ void put4(T16* y, const f32x4_t& v) {
+    T16 o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) put(o + e, v[e]);
+    uint2 u;
+    __builtin_memcpy(&u, o, 8);
+    *reinterpret_cast<uint2*>(y) = u;
+}
 
-// ---- few tokens: the weights are streamed once ----------------------------------------------
-// Work-group: 16 weight rows and up to 16 NT tokens; its waves take the scale blocks in turn.
-constexpr int kWaves = 4;
+// ---- up to 16 tokens: the weights are streamed once -----------------------------------------
+// Work-group: 16 weight rows and all the tokens; its 8 waves take the scale blocks in turn. Lane
+// (i, g) holds chunks g and 4 + g of row i of both operands (which columns a lane holds is free as
+// long as both agree), so that the two loads of a row's 128 bytes cover 64 contiguous bytes each.
+// 8 waves of one block a turn: 4096 x 11008 weights, one token 11.9 us (4 waves of two blocks 18,
+// 16 of one 11.0); 16 tokens 13.6 us (20.0, 15.4); 4096 x 4096, one token 6.1 us (7.7, 6.3).
+constexpr int kRowWaves = 8;
 
-template <typename YT, int NT, bool EXACT>
-__global__ __launch_bounds__(kWaves * 64) void fp8_rows(
+template <typename YT, bool EXACT>
+__global__ __launch_bounds__(kRowWaves * 64) void fp8_rows(
     const uint8_t* __restrict__ x, const float* __restrict__ xs, int M, int K,
     const uint8_t* __restrict__ w, const float* __restrict__ ws, int N, YT* __restrict__ y) {
-    __shared__ f32x4_t red[kWaves * NT * 64];
+    __shared__ f32x4_t red[kRowWaves * 64];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = lane & 15, g = lane >> 4;
-    const int n0 = blockIdx.x * 16, m0 = blockIdx.y * 16 * NT;
+    const int i = lane & 15, g = lane >> 4;
+    const int n0 = blockIdx.x * 16;
     const int kb = (K + kBlk - 1) / kBlk;
-    // descriptors of the tile's own rows: 32-bit offsets hold whatever M and N are
+    // descriptors of the tile's own rows: 32-bit offsets hold whatever N is
     const auto wr = make_rsrc(w + (int64_t)n0 * K, (int64_t)min(16, N - n0) * K);
-    const int mt = min(16 * NT, M - m0);
-    const auto xr = make_rsrc(x + (int64_t)m0 * K, (int64_t)mt * K);
+    const auto xr = make_rsrc(x, (int64_t)M * K);
+    const auto sr = make_rsrc(xs, (int64_t)M * kb * 4);
     const float* wsc = ws + (int64_t)(n0 / kBlk) * kb;
-    f32x4_t acc[NT];
+    // (rows past the last lie past their descriptor's end and read zeros)
+    const int ro = i * K + 16 * g, so = i * kb * 4;
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int b = wave; b < kb; b += kRowWaves) {
+        V16 a[2], v[2];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) acc[n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    const int wo = n0 + row < N ? row * K : kOOB;
-    int xo[NT];
-    const float* xsc[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) {
-        const int t = 16 * n + row;
-        xo[n] = t < mt ? t * K : kOOB;
-        xsc[n] = xs + (int64_t)(m0 + min(t, mt - 1)) * kb;
-    }
-    for (int b = wave; b < kb; b += kWaves) {
-        const int o = b * kBlk + 32 * g;
-        const auto a = Op<EXACT>::make(bload16(wr, (o < K) & (wo >= 0) ? wo + o : kOOB),
-                                       bload16(wr, (o + 16 < K) & (wo >= 0) ? wo + o + 16 : kOOB));
-        const float sw = wsc[b];
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-            const auto v =
-                Op<EXACT>::make(bload16(xr, (o < K) & (xo[n] >= 0) ? xo[n] + o : kOOB),
-                                bload16(xr, (o + 16 < K) & (xo[n] >= 0) ? xo[n] + o + 16 : kOOB));
-            const f32x4_t t = Op<EXACT>::mma(a, v);
-            const float s = sw * xsc[n][b];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) acc[n][i] = fmaf(s, t[i], acc[n][i]);
+        for (int h = 0; h < 2; ++h) {
+            const int o = b * kBlk + 64 * h;
+            const bool in = o + 16 * g < K;
+            a[h] = bload16(wr, in ? ro + o : kOOB);
+            v[h] = bload16(xr, in ? ro + o : kOOB);
         }
-    }
+        const float sx = __builtin_bit_cast(
+            float, __builtin_amdgcn_raw_buffer_load_b32(sr, so + 4 * b, 0, 0));
+        const f32x4_t t =
+            Op<EXACT>::mma(Op<EXACT>::make(a[0], a[1]), Op<EXACT>::make(v[0], v[1]));
+        const float f = sx * wsc[b];
 #pragma unroll
-    for (int n = 0; n < NT; ++n) red[(wave * NT + n) * 64 + lane] = acc[n];
+        for (int e = 0; e < 4; ++e) acc[e] = fmaf(f, t[e], acc[e]);
+    }
+    red[wave * 64 + lane] = acc;
     __syncthreads();
-    for (int n = wave; n < NT; n += kWaves) {
-        f32x4_t s = red[n * 64 + lane];
+    if (wave > 0) return;
+    f32x4_t s = red[lane];
 #pragma unroll
-        for (int v = 1; v < kWaves; ++v) {
-            const f32x4_t p = red[(v * NT + n) * 64 + lane];
+    for (int v = 1; v < kRowWaves; ++v) {
+        const f32x4_t p = red[v * 64 + lane];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] += p[i];
+        for (int e = 0; e < 4; ++e) s[e] += p[e];
+    }
+    if (i < M) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = n0 + 4 * g + e;
+            if (c < N) put(y + (int64_t)i * N + c, s[e]);
         }
-        const int t = 16 * n + row;
-        if (t < mt) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int c = n0 + 4 * g + i;
-                if (c < N) put(y + (int64_t)(m0 + t) * N + c, s[i]);
+    }
+}
+
+// ---- many tokens: LDS tiles --------------------------------------------------------------------
+// An item is a tile of BN weight rows x BM tokens over a run of scale blocks; WN x WM waves of TN x
+// TM each. A K step is one scale block: 128 bytes of every row and the tokens' scales, loaded
+// straight into one of S LDS stages, S steps ahead. Chunk c of row r lies at c ^ (r % 8), so that
+// neither the loads nor the 16-row operand reads conflict. A step's products leave the MFMA from
+// zero and are scaled into the total by vector instructions beside the next products: four FMAs for
+// each 16 x 16 x 128 product, half of its MFMA time.
+//
+// A work-group takes items in turn (grid: what the chip holds at once), and the loads run on into
+// the next item before an item's results are stored.
+struct Item {
+    int id;  // -1: past the last
+    int tm, tn, b0, b1;
+};
+
+template <int BN, int BM, int WN, int WM, int S, typename YT, bool EXACT, bool SPLIT>
+__global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
+    const uint8_t* __restrict__ x, const float* __restrict__ xs, int M, int K,
+    const uint8_t* __restrict__ w, const float* __restrict__ ws, int N, int ntm, int ntn, int items,
+    int per, YT* __restrict__ y) {
+    constexpr int NW = WN * WM, TN = BN / WN, TM = BM / WM, RN = TN / 16, RM = TM / 16;
+    constexpr int LA = BN / 8 / NW, LB = BM / 8 / NW;  // 8-row loads of a wave
+    static_assert(LA * NW * 8 == BN && LB * NW * 8 == BM && TN <= kBlk && kBlk % TN == 0, "tile");
+    static_assert(S >= 2 && S <= 4 && BM % 64 == 0 && RN % 2 == 0, "stages");
+    constexpr int kScale = (BN + BM) * kBlk;      // the tokens' scales behind the rows
+    constexpr int kStage = kScale + BM * 4;
+    // one array a stage: the compiler must see that a step's reads and loads do not alias, or it
+    // waits for the loads it has just issued
+    __shared__ __align__(1024) char s0[kStage];
+    __shared__ __align__(1024) char s1[kStage];
+    __shared__ __align__(1024) char s2[S > 2 ? kStage : 16];
+    __shared__ __align__(1024) char s3[S > 3 ? kStage : 16];
+    constexpr bool TOUCH = S == 2;  // deeper stages look far enough ahead by themselves
+    __shared__ __align__(256) char touched[TOUCH ? NW * 256 : 16];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = wave / WM, wm = wave - wn * WM;
+    const int i = lane & 15, g = lane >> 4;
+    const int kb = (K + kBlk - 1) / kBlk;
+
+    // item id of the grid's order: K chunk id / padded tiles, tile as the XCDs take them
+    const int ntp = (ntm * ntn + 7) / 8 * 8;
+    auto item_at = [&](int id) {
+        Item c;
+        for (; id < items; id += (int)gridDim.x) {
+            const int ks = SPLIT ? id / ntp : 0;
+            if (xcd_tile(id - ks * ntp, ntm, ntn, c.tm, c.tn)) {
+                c.id = id;
+                c.b0 = SPLIT ? ks * per : 0;
+                c.b1 = SPLIT ? min(kb, c.b0 + per) : kb;
+                return c;
             }
         }
+        c.id = -1;
+        c.tm = c.tn = c.b0 = 0;
+        c.b1 = 1;
+        return c;
+    };
+    // rounds of the stages that an item takes (the steps past its last load zeros); at least one
+    auto rounds = [&](const Item& c) { return (c.b1 - c.b0 + S - 1) / S; };
+
+    // This lane's part of an 8-row load: row lane / 8, chunk (lane % 8) ^ (row % 8). Rows past
+    // the item's last lie past its descriptor's end and read zeros. LDS row 16 n + i holds weight
+    // row 32 (n / 2) + 8 (i / 4) + 4 (n % 2) + i % 4, so that a lane's results of two row tiles
+    // are 8 consecutive columns of y.
+    const int lrow = lane >> 3, lcol = ((lane & 7) ^ lrow) * 16;
+    int va[LA], vb[LB];
+#pragma unroll
+    for (int t = 0; t < LA; ++t) {
+        const int r = (wave * LA + t) * 8 + lrow, p = r & 31;
+        va[t] = ((r & ~31) + 8 * ((p & 15) >> 2) + 4 * (p >> 4) + (p & 3)) * K + lcol;
+    }
+#pragma unroll
+    for (int t = 0; t < LB; ++t) vb[t] = ((wave * LB + t) * 8 + lrow) * K + lcol;
+    // every wave loads 64 tokens' scales (more than one wave the same ones where BM < 64 NW), so
+    // that all count the same loads
+    const int sg = wave % (BM / 64);
+    const int vs = (64 * sg + lane) * kb * 4;
+
+    // The tiles that an XCD works on at a time read the same rows in step, so that each step's
+    // lines would be first read, by all of them, one step before their use. Each of them also
+    // touches its share of the lines of a later step (one word a line, into LDS that nothing
+    // reads), which then come from the XCD's L2.
+    const int sharew = min(8, ntm), sharex = max(1, 32 / sharew);
+    const int rx = (BM + sharex - 1) / sharex, rw = (BN + sharew - 1) / sharew;
+    constexpr int kLoads = LA + LB + (TOUCH ? 2 : 1);
+    // what the loads read: rows of one item, from step lb on
+    __amdgpu_buffer_rsrc_t lw, lx, ls;
+    const uint8_t* pf;
+    int lb, lb1;
+    auto aim = [&](const Item& c) {
+        const int n0 = c.tn * BN, m0 = c.tm * BM;
+        // past the last item: descriptors of no bytes
+        const int nr = c.id < 0 ? 0 : min(BN, N - n0), mr = c.id < 0 ? 0 : min(BM, M - m0);
+        lw = make_rsrc(w + (int64_t)n0 * K, (int64_t)nr * K);
+        lx = make_rsrc(x + (int64_t)m0 * K, (int64_t)mr * K);
+        ls = make_rsrc(xs + (int64_t)m0 * kb, (int64_t)mr * kb * 4);
+        const int q = (int)threadIdx.x;
+        const int rr = min((c.tn % sharex) * rx + q, max(mr - 1, 0));
+        const int rs = min((c.tm % sharew) * rw + max(min(q - rx, rw - 1), 0), max(nr - 1, 0));
+        pf = q < rx ? x + (int64_t)(m0 + rr) * K : w + (int64_t)(n0 + rs) * K;
+        lb = c.b0;
+        lb1 = c.b1;
+    };
+    auto load = [&](char* at) {
+        typedef __attribute__((address_space(1))) const void global_void;
+        // columns past K (the last block of a ragged K) and steps past the run read zeros
+        const bool in = (lb < lb1) & (lb * kBlk + lcol < K);
+#pragma unroll
+        for (int t = 0; t < LA; ++t)
+            load_lds16(lw, at + (wave * LA + t) * 1024, in ? va[t] : kOOB, lb * kBlk);
+#pragma unroll
+        for (int t = 0; t < LB; ++t)
+            load_lds16(lx, at + BN * kBlk + (wave * LB + t) * 1024, in ? vb[t] : kOOB, lb * kBlk);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(ls, (lds_void*)(at + kScale + sg * 256), 4,
+                                                 lb < lb1 ? vs : kOOB, lb * 4, 0, 0);
+        if (TOUCH)
+            __builtin_amdgcn_global_load_lds((global_void*)(pf + min(lb + 1, lb1 - 1) * kBlk),
+                                             (lds_void*)(touched + wave * 256), 4, 0, 0);
+        ++lb;
+    };
+    f32x4_t acc[RN][RM];
+    // operand reads: row i of a tile, chunks g and 4 + g
+    const int o0 = i * kBlk + (g ^ (i & 7)) * 16, o1 = o0 ^ 64;
+    const int oa = wn * TN * kBlk, ob = BN * kBlk + wm * TM * kBlk;
+    const int os = kScale + (wm * TM + i) * 4;
+
+    // A step meets its barrier before the products of its last row tile: by then every wave has
+    // read the whole stage, so the loads of S steps on may overwrite it, and the next step's
+    // first operands are read under those products.
+    typename Op<EXACT>::type vx[RM];
+    V16 xlo[RM], xhi[RM], lo[2], hi[2];
+    f32x4_t t[2][RM];
+    float sc[RM], sp[RM], sraw[RM], sw, swn;
+    auto row_tile = [&](const char* at, int n) {
+        lo[n & 1] = ld16(at + oa + n * 16 * kBlk + o0);
+        hi[n & 1] = ld16(at + oa + n * 16 * kBlk + o1);
+    };
+    auto tokens = [&](const char* at, int m) {
+        xlo[m] = ld16(at + ob + m * 16 * kBlk + o0);
+        xhi[m] = ld16(at + ob + m * 16 * kBlk + o1);
+        sraw[m] = *reinterpret_cast<const float*>(at + os + 64 * m);
+    };
+    auto add = [&](int n, int m, const float* f) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[n][m][e] = fmaf(f[m], t[n & 1][m][e], acc[n][m][e]);
+    };
+    int wnext;  // index of the weights' scale of the step after this one
+    auto step = [&](char* cur, const char* nxt) {
+#pragma unroll
+        for (int m = 0; m < RM; ++m) {
+            vx[m] = Op<EXACT>::make(xlo[m], xhi[m]);
+            sp[m] = sc[m];
+            sc[m] = sraw[m] * sw;
+        }
+        swn = ws[wnext];
+#pragma unroll
+        for (int n = 0; n < RN; ++n) {
+            const bool last = n + 1 == RN;
+            if (last) {
+                wait_vm_lds<(S - 2) * kLoads + (TOUCH ? 1 : 0)>();
+                wg_barrier();
+                __builtin_amdgcn_sched_barrier(0);
+                load(cur);
+            }
+            const auto vw = Op<EXACT>::make(lo[n & 1], hi[n & 1]);
+            row_tile(last ? nxt : cur, last ? 0 : n + 1);
+#pragma unroll
+            for (int m = 0; m < RM; ++m) {
+                const f32x4_t v = Op<EXACT>::mma(vw, vx[m]);
+                // the products of the row tile before (of the step before, for the first)
+                if (n > 0)
+                    add(n - 1, m, sc);
+                else
+                    add(RN - 1, m, sp);
+                t[n & 1][m] = v;
+                if (last) tokens(nxt, m);
+            }
+            if (!EXACT) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+#pragma unroll
+                for (int m = 0; m < RM; ++m) {
+                    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                    if (last) __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x002, 4, 0);
+                }
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        sw = swn;
+    };
+    auto wscale = [&](const Item& c) {
+        return __builtin_amdgcn_readfirstlane((min(c.tn * BN + wn * TN, N - 1) / kBlk) * kb + c.b0);
+    };
+    Item it = item_at((int)blockIdx.x);
+    if (it.id < 0) return;
+    aim(it);
+    load(s0);
+    load(s1);
+    if (S > 2) load(s2);
+    if (S > 3) load(s3);
+    wnext = wscale(it);
+    sw = ws[wnext];
+    wait_vm_lds<(S - 1) * kLoads + (TOUCH ? 1 : 0)>();
+    wg_barrier();
+    row_tile(s0, 0);
+#pragma unroll
+    for (int m = 0; m < RM; ++m) tokens(s0, m);
+    while (true) {
+#pragma unroll
+        for (int m = 0; m < RM; ++m) {
+            sc[m] = 0.0f;
+            t[(RN - 1) & 1][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int n = 0; n < RN; ++n) acc[n][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        const Item next = item_at(it.id + (int)gridDim.x);
+        const int wthen = wscale(next), wlast = wnext + (it.b1 - it.b0 - 1);
+        int steps = rounds(it) * S;
+        auto one = [&](char* cur, const char* nxt) {
+            --steps;
+            wnext = steps == 0 ? wthen : (wnext < wlast ? wnext + 1 : wnext);
+            step(cur, nxt);
+        };
+        while (steps > 0) {
+            if (steps == S) aim(next);  // the last round's loads are the next item's first
+            one(s0, s1);
+            one(s1, S == 2 ? s0 : s2);
+            if (S > 2) one(s2, S == 3 ? s0 : s3);
+            if (S > 3) one(s3, s0);
+        }
+#pragma unroll
+        for (int m = 0; m < RM; ++m) add(RN - 1, m, sc);
+        // no load may land in LDS after the work-group's end (these are the ones of no item)
+        if (next.id < 0) wait_vm_lds<0>();
+        YT* const out = SPLIT ? y + (int64_t)(it.id / ntp) * M * N : y;
+#pragma unroll
+        for (int m = 0; m < RM; ++m) {
+            const int tk = it.tm * BM + wm * TM + 16 * m + i;
+            if (tk >= M) continue;
+#pragma unroll
+            for (int n = 0; n < RN; n += 2) {
+                const int c = it.tn * BN + wn * TN + 16 * n + 8 * g;
+                if ((N & 7) == 0) {
+                    if (c < N) put8(out + (int64_t)tk * N + c, acc[n][m], acc[n + 1][m]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (c + e < N)
+                            put(out + (int64_t)tk * N + c + e,
+                                e < 4 ? acc[n][m][e] : acc[n + 1][m][e - 4]);
+                }
+            }
+        }
+        if (next.id < 0) break;
+        it = next;
+    }
+}
+
+// y = the sum of the K chunks' partial products, in order
+template <typename YT>
+__global__ __launch_bounds__(256) void fp8_sum(const float* __restrict__ part, int ks, int64_t n,
+                                               YT* __restrict__ y) {
+    const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (at + 4 <= n && (n & 3) == 0) {
+        f32x4_t s = *reinterpret_cast<const f32x4_t*>(part + at);
+        for (int k = 1; k < ks; ++k) {
+            const f32x4_t v = *reinterpret_cast<const f32x4_t*>(part + k * n + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) s[e] += v[e];
+        }
+        put4(y + at, s);
+    } else {
+        for (int e = 0; e < 4; ++e) {
+            if (at + e >= n) return;
+            float s = part[at + e];
+            for (int k = 1; k < ks; ++k) s += part[k * n + at + e];
+            put(y + at + e, s);
+        }
+    }
+}
+
+// Tiles by number, the largest first: rows x tokens, stages, work-groups that fit a CU
+struct Tile {
+    int bn, bm;
+};
+constexpr Tile kTiles[] = {{256, 256}, {256, 128}, {128, 128}, {128, 64}, {64, 64}};
+constexpr int kNumTiles = 5;
+
+struct Fp8Plan {
+    int tile;  // -1: fp8_rows
+    int ks;    // K chunks, none of them empty
+    int per;   // blocks a chunk
+};
+
+// Weights of few rows and up to 16 tokens: fp8_rows. From 160 tiles of 64 rows on the 64 x 64 tile
+// streams them as fast and reads x once for 64 rows instead of 16 (14336 x 4096: one token 15.1 us
+// by rows and 14.4 by tiles, 16 tokens 22.5 and 15.3; 4096 x 4096, 64 tiles: 6.1 and 10.4, 7.4 and
+// 10.9); a float32 result spends its tiles' time on widening codes of padding, so up to 4 tokens
+// stay with the rows (15.3 and 18.6).
+// Otherwise the largest tile of which there are about as many as CUs, K split in up to 4 chunks of
+// at least 20 blocks for it (partial sums cost as much as a few blocks): 14336 x 4096, 1024 tokens
+// 68 us by 256 x 256, 95 by 256 x 128 or 128 x 128; 512 tokens 51 us by 256 x 128, 66 by 256 x 256
+// and 60 with two chunks of 16 blocks; 4096 x 11008, 512 tokens 46.9 us by 128 x 128 in two chunks,
+// 54 by 128 x 64. The smallest tile takes any split that fills the chip: 4096 x 11008, 32 tokens
+// 25 us in one chunk, 14.8 in four.
+// The 256 x 256 tile's registers do not hold widened codes (EXACT).
+Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
+    const int kb = (int)((K + kBlk - 1) / kBlk);
+    if (M <= 16 && ((N + 63) / 64 < 160 || (exact && M <= 4))) return {-1, 1, kb};
+    constexpr int64_t kFull = 200;
+    for (int t = exact ? 1 : 0; t < kNumTiles; ++t) {
+        const int64_t n = ((N + kTiles[t].bn - 1) / kTiles[t].bn) *
+                          ((M + kTiles[t].bm - 1) / kTiles[t].bm);
+        const bool smallest = t + 1 == kNumTiles;
+        for (int ks = 1; ks <= 4; ks *= 2) {
+            if (ks > 1 && kb / ks < (smallest ? 8 : 20)) break;
+            const bool most = smallest && (ks == 4 || kb / (2 * ks) < 8);
+            if (n * ks >= kFull || most) {
+                const int per = (kb + ks - 1) / ks;
+                return {t, (kb + per - 1) / per, per};
+            }
+        }
+    }
+    return {kNumTiles - 1, 1, kb};
+}
+
+template <int T, int WN, int WM, int S, typename YT, bool EXACT>
+void tiles(const Fp8Plan& p, const uint8_t* x, const float* xs, int64_t M, int64_t K,
+           const uint8_t* w, const float* ws, int64_t N, YT* y, float* part, hipStream_t s) {
+    constexpr int BN = kTiles[T].bn, BM = kTiles[T].bm;
+    const int ntm = (int)((M + BM - 1) / BM), ntn = (int)((N + BN - 1) / BN);
+    const int64_t items = ((int64_t)ntm * ntn + 7) / 8 * 8 * p.ks;
+    constexpr int kFit = S * ((BN + BM) * kBlk + BM * 4) > 80000 ? 1 : 2;  // by LDS
+    const int64_t most = (int64_t)current_cu_count() * kFit;
+    const unsigned grid = (unsigned)(items < most ? items : most);
+    if (p.ks == 1) {
+        fp8_tiles<BN, BM, WN, WM, S, YT, EXACT, false><<<dim3(grid), WN * WM * 64, 0, s>>>(
+            x, xs, (int)M, (int)K, w, ws, (int)N, ntm, ntn, (int)items, p.per, y);
+    } else {
+        fp8_tiles<BN, BM, WN, WM, S, float, EXACT, true><<<dim3(grid), WN * WM * 64, 0, s>>>(
+            x, xs, (int)M, (int)K, w, ws, (int)N, ntm, ntn, (int)items, p.per, part);
+        fp8_sum<YT><<<dim3((unsigned)((M * N + 1023) / 1024)), 256, 0, s>>>(part, p.ks, M * N, y);
     }
 }
 
 template <typename YT>
 void run(const uint8_t* x, const float* xs, int64_t M, int64_t K, const uint8_t* w,
-         const float* ws, int64_t N, YT* y, hipStream_t s) {
+         const float* ws, int64_t N, YT* y, float* part, hipStream_t s) {
     constexpr bool EXACT = sizeof(YT) == 4;
-    const unsigned gn = (unsigned)((N + 15) / 16);
-    if (M <= 16)
-        fp8_rows<YT, 1, EXACT><<<dim3(gn), kWaves * 64, 0, s>>>(x, xs, (int)M, (int)K, w, ws, (int)N, y);
-    else
-        fp8_rows<YT, 4, EXACT><<<dim3(gn, (unsigned)((M + 63) / 64)), kWaves * 64, 0, s>>>(
-            x, xs, (int)M, (int)K, w, ws, (int)N, y);
+    const Fp8Plan p = fp8_plan(M, N, K, EXACT);
+    switch (p.tile) {
+        case -1:
+            fp8_rows<YT, EXACT><<<dim3((unsigned)((N + 15) / 16)), kRowWaves * 64, 0, s>>>(
+                x, xs, (int)M, (int)K, w, ws, (int)N, y);
+            break;
+        case 0:
+            if constexpr (!EXACT)
+                tiles<0, 2, 4, 2, YT, EXACT>(p, x, xs, M, K, w, ws, N, y, part, s);
+            break;
+        case 1: tiles<1, 4, 2, 3, YT, EXACT>(p, x, xs, M, K, w, ws, N, y, part, s); break;
+        case 2: tiles<2, 2, 2, 2, YT, EXACT>(p, x, xs, M, K, w, ws, N, y, part, s); break;
+        case 3: tiles<3, 4, 1, 3, YT, EXACT>(p, x, xs, M, K, w, ws, N, y, part, s); break;
+        default: tiles<4, 2, 2, 4, YT, EXACT>(p, x, xs, M, K, w, ws, N, y, part, s); break;
+    }
 }
 
 }  // namespace
 
-size_t fp8_workspace(int64_t M, int64_t N, int64_t K) { return 0; }
+// plan[0..1]: rows and tokens of the tile (0, 0: fp8_rows), plan[2]: K chunks
+void fp8_tiles_of(int64_t M, int64_t N, int64_t K, int ydt, int32_t* plan) {
+    const Fp8Plan p = fp8_plan(M, N, K, ydt == 0);
+    plan[0] = p.tile < 0 ? 0 : kTiles[p.tile].bn;
+    plan[1] = p.tile < 0 ? 0 : kTiles[p.tile].bm;
+    plan[2] = p.ks;
+}
+
+// partial sums of a split K (the plans of the two kinds of output may differ)
+size_t fp8_workspace(int64_t M, int64_t N, int64_t K) {
+    const int a = fp8_plan(M, N, K, false).ks, b = fp8_plan(M, N, K, true).ks;
+    const int ks = a > b ? a : b;
+    return ks > 1 ? (size_t)ks * M * N * sizeof(float) : 0;
+}
 
 hipError_t launch_matmul_fp8(const uint8_t* x, const float* xs, int64_t M, int64_t K,
                              const uint8_t* w, const float* ws, int64_t N, void* y, int ydt,
                              void* wsp, hipStream_t s) {
+    float* part = static_cast<float*>(wsp);
     if (ydt == 0)
-        run(x, xs, M, K, w, ws, N, static_cast<float*>(y), s);
+        run(x, xs, M, K, w, ws, N, static_cast<float*>(y), part, s);
     else if (ydt == 1)
-        run(x, xs, M, K, w, ws, N, static_cast<bf16_t*>(y), s);
+        run(x, xs, M, K, w, ws, N, static_cast<bf16_t*>(y), part, s);
     else
-        run(x, xs, M, K, w, ws, N, static_cast<f16_t*>(y), s);
+        run(x, xs, M, K, w, ws, N, static_cast<f16_t*>(y), part, s);
     return hipGetLastError();
 }
 

@@ -156,6 +156,7 @@ int64_t quant_groups(int64_t G, int64_t R, int64_t C, int block_rows);
 hipError_t launch_quant(const void* x, int xdt, int64_t G, int64_t R, int64_t C, int block_rows,
                         uint8_t* codes, float* scales, hipStream_t s);
 size_t fp8_workspace(int64_t M, int64_t N, int64_t K);
+void fp8_tiles_of(int64_t M, int64_t N, int64_t K, int ydt, int32_t* plan);
 hipError_t launch_matmul_fp8(const uint8_t* x, const float* xs, int64_t M, int64_t K,
                              const uint8_t* w, const float* ws, int64_t N, void* y, int ydt,
                              void* wsp, hipStream_t s);

@@ -101,6 +101,28 @@ def test_workspace_queries(lib):  # noqa: F811
     assert lib.si_moe_layer_workspace(0, 2, 8, 64, 48, BF16, BF16, F32) == 0
 
 
+def test_every_tile_is_value_checked(lib):  # noqa: F811
+    """The sizes of the GPU tests reach every tile of the 8-bit product, each with and without K
+    chunks, for float32 and 16-bit results."""
+    import paper_2607_18081_amd as si
+    from tests.test_gpu_fp8 import LARGE, NAMES
+    seen = {(dt == "f32", *si.matmul_fp8_plan(M, N, K, NAMES[dt])) for M, N, K, dt in LARGE}
+    for exact in (False, True):
+        tiles = [(256, 256), (256, 128), (128, 128), (128, 64), (64, 64)][exact:]
+        for t in tiles:
+            assert any(s[:3] == (exact, *t) for s in seen), (exact, t)
+        assert any(s[0] == exact and s[3] > 1 for s in seen)
+    assert {s[1:3] for s in seen if s[3] > 1} >= {(256, 256), (256, 128), (128, 128), (64, 64)}
+    assert si.matmul_fp8_plan(1, 4096, 4096)[0] == 0
+    for M in (1, 5, 17, 64, 200, 1000, 5000):
+        for N in (1, 100, 3000, 20000):
+            for K in (16, 1000 * 16, 128 * 37):
+                for dt in NAMES.values():
+                    ks = si.matmul_fp8_plan(M, N, K, dt)[2]
+                    assert 1 <= ks <= 4
+                    assert lib.si_matmul_fp8_workspace(M, N, K) >= (ks > 1) * ks * M * N * 4
+
+
 # ---- refusals --------------------------------------------------------------------------------
 
 @pytest.fixture(scope="module")

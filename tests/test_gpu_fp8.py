@@ -115,6 +115,38 @@ def test_matmul(M, N, K, dtype):
     assert torch.equal(again, y)                             # bitwise repeatable
 
 
+# sizes that reach every tile, with and without K chunks, at ragged edges: 64 tokens are compared
+LARGE = [
+    (4010, 3401, 400, "bf16"), (2050, 3500, 272, "f16"), (1001, 4000, 5264, "bf16"),
+    (1500, 3400, 144, "bf16"), (2047, 3390, 400, "f32"), (700, 3990, 5200, "bf16"),
+    (1030, 3333, 272, "f32"), (900, 3333, 272, "bf16"), (511, 4095, 5136, "f32"),
+    (500, 3333, 656, "bf16"), (500, 3333, 656, "f32"), (120, 6001, 5216, "bf16"),
+    (1500, 5000, 5264, "bf16"), (250, 3400, 400, "bf16"), (250, 3400, 400, "f32"),
+    (60, 4000, 4112, "f16"),
+    (60, 4000, 2064, "f32"), (9, 10500, 272, "bf16"), (9, 10500, 400, "f32"),
+]
+NAMES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+@pytest.mark.parametrize("M,N,K,dt", LARGE)
+def test_matmul_tiles(M, N, K, dt):
+    say(f"matmul tiles M={M} N={N} K={K} {dt} {si.matmul_fp8_plan(M, N, K, NAMES[dt])}")
+    rng = np.random.default_rng(M + N + K)
+    nk = -(-K // 128)
+    table = oracle.encode_e4m3(np.clip(rng.normal(0, 120, 1 << 16), -448, 448))
+    x, w = table[rng.integers(0, 1 << 16, (M, K))], table[rng.integers(0, 1 << 16, (N, K))]
+    xs = np.exp(rng.normal(-4, 1, (M, nk))).astype(np.float32)
+    ws = np.exp(rng.normal(-8, 1, (-(-N // 128), nk))).astype(np.float32)
+    args = [_dev(a) for a in (x, xs, w, ws)]
+    need = si._lib.load().si_matmul_fp8_workspace(M, N, K)
+    space = torch.full((max(need, 16),), 0xff, dtype=torch.uint8, device=DEV)    # NaN bits
+    out = torch.full((M, N), float("nan"), dtype=NAMES[dt], device=DEV)
+    y = si.matmul_fp8(*args, out_dtype=NAMES[dt], out=out, workspace=space)
+    rows = np.unique(np.concatenate([[0, M - 1], rng.integers(0, M, 62)]))
+    _check(y[torch.from_numpy(rows).to(DEV)], x[rows], xs[rows], w, ws, NAMES[dt])
+    assert torch.equal(si.matmul_fp8(*args, out_dtype=NAMES[dt]), y)
+
+
 @pytest.mark.parametrize("M", [3, 70, 300])
 def test_matmul_nan_stays_in_its_row(M):
     """A token quantised from a NaN is NaN, and so is a weight row; the rest is as without."""
