@@ -22,12 +22,12 @@
 #include "common.h"
 #include "launch.h"
 #include "mfma.h"
+#include "pipe.h"
 
 namespace si {
 
 namespace {
 
-constexpr int kWaves = 4;           // a work-group's waves, which split K
 constexpr int kLine = 128;          // bytes of a weight row a wave takes at a step
 constexpr int kMaxNT = 4;           // token tiles of 16 served by one pass over the weights
 
@@ -82,7 +82,8 @@ struct Core<XT, true> {
 // The pairs of this work-group's expert, ascending, into list[]; their number. Every thread of
 // the work-group calls it. by_pair: the grid's slot is a pair, and the work-group serves that
 // pair's expert only if no earlier pair has it (else 0); otherwise the slot is the expert.
-__device__ int expert_pairs(const int32_t* __restrict__ ids, int npairs, int E, int slot,
+template <int W>
+__device__ __forceinline__ int expert_pairs(const int32_t* __restrict__ ids, int npairs, int E, int slot,
                             int by_pair, int& e, uint16_t* list, int* cnt) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -92,7 +93,7 @@ __device__ int expert_pairs(const int32_t* __restrict__ ids, int npairs, int E, 
         if ((unsigned)e >= (unsigned)E) return 0;
     }
     // wave w scans a run of the pairs: count, then place after the earlier waves' pairs
-    const int per = ((npairs + kWaves - 1) / kWaves + 63) / 64 * 64;
+    const int per = ((npairs + W - 1) / W + 63) / 64 * 64;
     const int lo = wave * per, hi = min(npairs, lo + per);
     int n = 0;
     bool earlier = false;
@@ -105,9 +106,9 @@ __device__ int expert_pairs(const int32_t* __restrict__ ids, int npairs, int E, 
     if (__syncthreads_or(earlier)) return 0;
     int at = 0, total = 0;
 #pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-        if (w < wave) at += cnt[w];
-        total += cnt[w];
+    for (int v = 0; v < W; ++v) {
+        if (v < wave) at += cnt[v];
+        total += cnt[v];
     }
     for (int b = lo; b < hi; b += 64) {
         const bool hit = b + lane < hi && ids[b + lane] == e;
@@ -119,91 +120,157 @@ __device__ int expert_pairs(const int32_t* __restrict__ ids, int npairs, int E, 
     return __builtin_amdgcn_readfirstlane(total);
 }
 
-// acc[r][n] += the product of RT row tiles and NT token tiles over this wave's lines.
-//   wr, woff[r]   the expert's weights and the byte offset of this lane's row of tile r (kOOB:
-//                 no such row), rb the bytes of a row
-//   xr, xoff[n]   the token operand (PARTS planes, `plane` bytes apart) and the byte offset of
-//                 this lane's token row of tile n (kOOB: none); xb its bytes
+// LDS reads of operand tiles: 16 bytes at addr0 + O and at addr1 + O for each of N tiles 2048 bytes
+// apart, waited for in place. (Not ordinary loads: the compiler would wait for every load into LDS
+// in flight before each of them, since it cannot tell the stages of a wave's ring apart.)
+template <int N, int O>
+__device__ __forceinline__ void lds_tiles(uint32_t addr0, uint32_t addr1, V16 (*out)[2]) {
+    u32x4_t v0, v1;
+    if constexpr (N == 1) {
+        asm volatile(
+            "ds_read_b128 %0, %2 offset:%4\n\t"
+            "ds_read_b128 %1, %3 offset:%4\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(v0), "=&v"(v1)
+            : "v"(addr0), "v"(addr1), "n"(O)
+            : "memory");
+    } else {
+        u32x4_t v2, v3;
+        asm volatile(
+            "ds_read_b128 %0, %4 offset:%6\n\t"
+            "ds_read_b128 %1, %5 offset:%6\n\t"
+            "ds_read_b128 %2, %4 offset:%7\n\t"
+            "ds_read_b128 %3, %5 offset:%7\n\t"
+            "s_waitcnt lgkmcnt(0)"
+            : "=&v"(v0), "=&v"(v1), "=&v"(v2), "=&v"(v3)
+            : "v"(addr0), "v"(addr1), "n"(O), "n"(O + 2048)
+            : "memory");
+        out[1][0] = __builtin_bit_cast(V16, v2);
+        out[1][1] = __builtin_bit_cast(V16, v3);
+    }
+    out[0][0] = __builtin_bit_cast(V16, v0);
+    out[0][1] = __builtin_bit_cast(V16, v1);
+    if constexpr (N > 2) lds_tiles<N - 2, O + 4096>(addr0, addr1, out + 2);
+}
+__device__ __forceinline__ uint32_t lds_addr(const char* p) {
+    return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+
+// 1 KB loads into LDS that one line takes: two of 8 rows for each row tile, and for each token
+// tile, part and 128 bytes of its columns
+template <bool FP8, int RT, int NT, int PARTS>
+constexpr int line_loads() {
+    return 2 * RT + 2 * NT * PARTS * (FP8 ? 2 : 1);
+}
+
+// acc[r][n] += the product of RT row tiles and NT token tiles over the lines [l0, l1).
+//   wr, woff[r]   the expert's weights and the byte offset of row lane / 8 of tile r, in woff[r][1]
+//                 that of row lane / 8 + 8 (kOOB: no such row); rb the bytes of a row
+//   xr, xoff[n]   the same for the token operand (PARTS planes, `plane` bytes apart), xb its bytes
 //   sc[r]         scales of tile r's rows, one a line (FP8)
-// Lane (i, g) of a wave holds row i of a tile and columns 16 g .. of each half line, of the
-// weights and of the tokens alike.
-template <typename XT, bool FP8, int RT, int NT, int PARTS, int U>
+//   ring          this wave's own LDS: D stages of line_loads() KB
+// A line goes from memory to LDS in whole 128-byte rows (8 rows a load), D lines ahead; chunk c of
+// row r lies at c ^ (r % 8), so that the 16-row reads do not conflict. Loads straight into
+// registers in the operand's shape, 64 bytes of 16 rows each, streamed at 3.4 to 4.4 TB/s. Lane
+// (i, g) takes chunks g and 4 + g of row i.
+template <typename XT, bool FP8, int RT, int NT, int PARTS, int D, int POL>
 __device__ __forceinline__ void lines(f32x4_t (&acc)[RT][NT], __amdgpu_buffer_rsrc_t wr,
-                                      const int (&woff)[RT], int rb, __amdgpu_buffer_rsrc_t xr,
-                                      const int (&xoff)[NT], int xb, int plane,
-                                      const float* const (&sc)[RT], int l0, int l1) {
+                                      const int (&woff)[RT][2], int rb, __amdgpu_buffer_rsrc_t xr,
+                                      const int (&xoff)[NT][2], int xb, int plane,
+                                      const float* const (&sc)[RT], int l0, int l1, char* ring) {
     using C = Core<XT, FP8>;
-    const int g = (threadIdx.x & 63) >> 4;
-    for (int l = l0; l < l1; l += U) {
-        V16 a[U][RT][2], b[U][NT][PARTS][2 * C::XC];
+    constexpr int XC = C::XC;
+    constexpr int L = line_loads<FP8, RT, NT, PARTS>();
+    static_assert(D >= 1 && (D - 1) * L <= 63, "outstanding loads");
+    const int lane = threadIdx.x & 63;
+    const int i = lane & 15, g = lane >> 4;
+    const int lcol = ((lane & 7) ^ (lane >> 3)) * 16;
+    auto load = [&](int l, char* at) {
+        // lines past the run and columns past the row read zeros
+        const bool in = (l < l1) & (l * kLine + lcol < rb);
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int o = (l + u) * kLine + 64 * h + 16 * g;
-                const bool in = (l + u < l1) & (o < rb);
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-                    a[u][r][h] = bload16(wr, (in & (woff[r] >= 0)) ? woff[r] + o : kOOB);
-            }
-#pragma unroll
-            for (int c = 0; c < 2 * C::XC; ++c) {
-                const int o = C::XC == 1 ? (l + u) * kLine + 64 * c + 16 * g
-                                         : (l + u) * 2 * kLine + 128 * (c >> 1) + 32 * g +
-                                               16 * (c & 1);
-                const bool in = (l + u < l1) & (o < xb);
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int p = 0; p < PARTS; ++p)
-                        b[u][n][p][c] =
-                            bload16(xr, (in & (xoff[n] >= 0)) ? xoff[n] + p * plane + o : kOOB);
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            f32x4_t blk[RT][NT];
-            if (FP8) {
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) blk[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-            }
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
+                load_lds16<POL>(wr, at + (2 * r + h) * 1024,
+                                (in & (woff[r][h] >= 0)) ? woff[r][h] + lcol : kOOB, l * kLine);
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    typename C::vec w[C::XC];
-                    C::widen(a[u][r][h], w);
+        for (int c = 0; c < XC; ++c) {
+            const int o = (l * XC + c) * kLine;
+            const bool xin = (l < l1) & (o + lcol < xb);
 #pragma unroll
-                    for (int c = 0; c < C::XC; ++c)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int n = 0; n < NT; ++n)
+                for (int p = 0; p < PARTS; ++p)
 #pragma unroll
-                            for (int p = 0; p < PARTS; ++p) {
-                                f32x4_t& t = FP8 ? blk[r][n] : acc[r][n];
-                                t = C::mma(w[c], b[u][n][p][h * C::XC + c], t);
-                            }
-                }
-            if (FP8 && l + u < l1) {
+                    for (int h = 0; h < 2; ++h)
+                        load_lds16(xr, at + (2 * RT + 2 * ((n * PARTS + p) * XC + c) + h) * 1024,
+                                   (xin & (xoff[n][h] >= 0)) ? xoff[n][h] + lcol : kOOB,
+                                   p * plane + o);
+        }
+    };
 #pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    const float s = sc[r][l + u];
+    for (int d = 0; d < D; ++d) load(l0 + d, ring + d * L * 1024);
+    const uint32_t base = lds_addr(ring) + i * kLine;
+    // positions of this lane's chunks: g and 4 + g, or, of the tokens of a code line, 2 g and
+    // 2 g + 1 of each half
+    const uint32_t a0 = base + (g ^ (i & 7)) * 16, a1 = base + ((4 + g) ^ (i & 7)) * 16;
+    const uint32_t x0 = XC == 1 ? a0 : base + ((2 * g) ^ (i & 7)) * 16;
+    const uint32_t x1 = XC == 1 ? a1 : base + ((2 * g + 1) ^ (i & 7)) * 16;
+    int slot = 0;
+    for (int l = l0; l < l1; ++l) {
+        wait_vm_lds<(D - 1) * L>();
+        V16 a[RT][2], b[NT * PARTS * XC][2];
+        const uint32_t at = slot * L * 1024;
+        lds_tiles<RT, 0>(a0 + at, a1 + at, a);
+        lds_tiles<NT * PARTS * XC, 2048 * RT>(x0 + at, x1 + at, b);
+        load(l + D, ring + at);
+        slot = slot + 1 == D ? 0 : slot + 1;
+        f32x4_t blk[RT][NT];
+        if (FP8) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) blk[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                typename C::vec w[XC];
+                C::widen(a[r][h], w);
+#pragma unroll
+                for (int c = 0; c < XC; ++c)
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            acc[r][n][i] = fmaf(s, blk[r][n][i], acc[r][n][i]);
-                }
+                        for (int p = 0; p < PARTS; ++p) {
+                            f32x4_t& t = FP8 ? blk[r][n] : acc[r][n];
+                            t = C::mma(w[c],
+                                       XC == 1 ? b[n * PARTS + p][h]
+                                               : b[(n * PARTS + p) * XC + h * (XC - 1)][c], t);
+                        }
+            }
+        if (FP8) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float s = sc[r][l];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[r][n][e] = fmaf(s, blk[r][n][e], acc[r][n][e]);
             }
         }
     }
+    wait_vm_lds<0>();  // the ring is free again
 }
 
-// lines of this wave: equal runs, in whole lines
-__device__ __forceinline__ void wave_lines(int nl, int wave, int& l0, int& l1) {
-    const int per = (nl + kWaves - 1) / kWaves;
-    l0 = min(nl, wave * per);
+// lines of a wave: equal runs, in whole lines
+template <int WK>
+__device__ __forceinline__ void wave_lines(int nl, int wk, int& l0, int& l1) {
+    const int per = (nl + WK - 1) / WK;
+    l0 = min(nl, wk * per);
     l1 = min(nl, l0 + per);
 }
 
@@ -246,103 +313,174 @@ __device__ __forceinline__ void put_h(float h, int64_t at, int64_t plane, int pa
     }
 }
 
-// ---- gate and up, SiLU(g) * u -> h ---------------------------------------------------------
-// Work-group: 16 neurons (their gate and up rows) of one expert.
-template <typename XT, bool FP8, int NT, int U>
-__device__ __forceinline__ void gate_up_pass(
-    const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
-    const uint16_t* list, int m, typename HType<XT, FP8>::type* H, int64_t plane, int parts,
-    f32x4_t* red) {
-    constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
-    const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = lane & 15, g = lane >> 4;
-    const int rb = d * WB;
-    const auto wr = make_rsrc(gu, (int64_t)2 * I * rb);
-    const auto xr = make_rsrc(x, xbytes);
-    int woff[2], xoff[NT];
-    woff[0] = n0 + row < I ? (n0 + row) * rb : kOOB;
-    woff[1] = n0 + row < I ? (I + n0 + row) * rb : kOOB;
+// LDS of a wave: its ring, which the sums of the waves reuse. Passes of 16, 32 and 64 tokens keep
+// as many lines in flight as fit it.
+template <int RING, bool FP8, int RT, int NT, int PARTS>
+constexpr int ring_depth() {
+    constexpr int by_lds = RING / 1024 / line_loads<FP8, RT, NT, PARTS>();
+    constexpr int by_count = 63 / line_loads<FP8, RT, NT, PARTS>() + 1;
+    constexpr int d = by_lds < by_count ? by_lds : by_count;
+    return d < 4 ? d : 4;
+}
+// token tiles a pass: 4, or what leaves two lines in flight
+template <int RING, bool FP8, int RT, int PARTS>
+constexpr int max_tiles() {
+    return ring_depth<RING, FP8, RT, 4, PARTS>() >= 2
+               ? 4
+               : (ring_depth<RING, FP8, RT, 2, PARTS>() >= 2 ? 2 : 1);
+}
+
+// Sums acc over the WK waves that split K of one row group, in order; on return out(q, s) has been
+// called for this wave's share of the NQ tiles, each with its sum.
+template <int WK, int NQ, typename F>
+__device__ __forceinline__ void join_waves(const f32x4_t* acc, f32x4_t* red, int wk, int lane,
+                                           F out) {
+    if constexpr (WK == 1) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-        xoff[n] = 16 * n + row < m ? (list[16 * n + row] / k) * d * (int)sizeof(XT) : kOOB;
-    const int nl = (rb + kLine - 1) / kLine;
-    const int nb = (I + 127) / 128;
-    const float* sc[2] = {nullptr, nullptr};
-    if (FP8) {
-        sc[0] = gus + (int64_t)(n0 / 128) * nl;
-        sc[1] = gus + (int64_t)(nb + n0 / 128) * nl;
-    }
-    int l0, l1;
-    wave_lines(nl, wave, l0, l1);
-    f32x4_t acc[2][NT];
+        for (int q = 0; q < NQ; ++q) out(q, acc[q]);
+    } else {
+        __syncthreads();  // the rings are done with
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
+        for (int q = 0; q < NQ; ++q) red[(wk * NQ + q) * 64 + lane] = acc[q];
+        __syncthreads();
+        for (int q = wk; q < NQ; q += WK) {
+            f32x4_t s = red[q * 64 + lane];
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    lines<XT, FP8, 2, NT, 1, U>(acc, wr, woff, rb, xr, xoff, d * (int)sizeof(XT), 0, sc, l0, l1);
-    __syncthreads();  // the last pass's reads of red are done
+            for (int w = 1; w < WK; ++w) {
+                const f32x4_t v = red[(w * NQ + q) * 64 + lane];
 #pragma unroll
-    for (int r = 0; r < 2; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) red[((wave * 2 + r) * NT + n) * 64 + lane] = acc[r][n];
-    __syncthreads();
-    // wave w finishes token tiles w, w + kWaves, ...
-    for (int n = wave; n < NT; n += kWaves) {
-        f32x4_t s[2];
-#pragma unroll
-        for (int r = 0; r < 2; ++r) {
-            s[r] = red[(r * NT + n) * 64 + lane];
-#pragma unroll
-            for (int w = 1; w < kWaves; ++w) {
-                const f32x4_t v = red[((w * 2 + r) * NT + n) * 64 + lane];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[r][i] += v[i];
+                for (int e = 0; e < 4; ++e) s[e] += v[e];
             }
+            out(q, s);
         }
-        // lane (i, g) holds token i, neurons 4 g ..
-        if (16 * n + row < m) {
-            const int64_t pair = list[16 * n + row];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int j = n0 + 4 * g + i;
-                if (j < I) put_h(silu_f32(s[0][i]) * s[1][i], pair * I + j, plane, parts, H);
-            }
-        }
+        __syncthreads();  // before the next pass's loads
     }
 }
 
-template <typename XT, bool FP8, int U>
-__global__ __launch_bounds__(kWaves * 64) void moe_gate_up(
+// ---- gate and up, SiLU(g) * u -> h ---------------------------------------------------------
+// Work-group: WR groups of 16 neurons (their gate and up rows) of one expert, K split over WK waves.
+template <typename XT, bool FP8, int RING, int WK, int NR, int NT>
+__device__ __forceinline__ void gate_up_pass(
+    const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
+    const uint16_t* list, int m, typename HType<XT, FP8>::type* H, int64_t plane, int parts, int wk,
+    char* ring, f32x4_t* red) {
+    constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
+    constexpr int RT = 2 * NR;  // tile 2 q: gate rows of neurons 16 q .., 2 q + 1: their up rows
+    constexpr int D = ring_depth<RING, FP8, RT, NT, 1>();
+    const int lane = threadIdx.x & 63;
+    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
+    const int rb = d * WB;
+    const auto wr = make_rsrc(gu, (int64_t)2 * I * rb);
+    const auto xr = make_rsrc(x, xbytes);
+    int woff[RT][2], xoff[NT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int j = n0 + 16 * (r >> 1) + 8 * h + lr;
+            woff[r][h] = j < I ? ((r & 1) * I + j) * rb : kOOB;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int t = 16 * n + 8 * h + lr;
+            xoff[n][h] = t < m ? (list[t] / k) * d * (int)sizeof(XT) : kOOB;
+        }
+    }
+    const int nl = (rb + kLine - 1) / kLine;
+    const int nb = (I + 127) / 128;
+    const float* sc[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+        sc[r] = FP8 ? gus + (int64_t)((r & 1) * nb + min(n0 + 16 * (r >> 1), I - 1) / 128) * nl
+                    : nullptr;
+    int l0, l1;
+    wave_lines<WK>(nl, wk, l0, l1);
+    f32x4_t acc[RT][NT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    lines<XT, FP8, RT, NT, 1, D, kNonTemporal>(acc, wr, woff, rb, xr, xoff, d * (int)sizeof(XT), 0,
+                                               sc, l0, l1, ring);
+    auto finish = [&](int q, const f32x4_t& sg, const f32x4_t& su) {
+        // lane (i, g) holds token i, neurons 4 g ..
+        const int nr = q / NT, n = q - nr * NT;
+        if (16 * n + row < m) {
+            const int64_t pair = list[16 * n + row];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = n0 + 16 * nr + 4 * g + e;
+                if (j < I) put_h(silu_f32(sg[e]) * su[e], pair * I + j, plane, parts, H);
+            }
+        }
+    };
+    constexpr int NQ = NR * NT;
+    if constexpr (WK == 1) {
+#pragma unroll
+        for (int q = 0; q < NQ; ++q) finish(q, acc[2 * (q / NT)][q % NT], acc[2 * (q / NT) + 1][q % NT]);
+    } else {
+        __syncthreads();  // the rings are done with
+#pragma unroll
+        for (int q = 0; q < NQ; ++q)
+#pragma unroll
+            for (int r = 0; r < 2; ++r)
+                red[((wk * NQ + q) * 2 + r) * 64 + lane] = acc[2 * (q / NT) + r][q % NT];
+        __syncthreads();
+        for (int q = wk; q < NQ; q += WK) {
+            f32x4_t s[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                s[r] = red[(q * 2 + r) * 64 + lane];
+#pragma unroll
+                for (int w = 1; w < WK; ++w) {
+                    const f32x4_t v = red[((w * NQ + q) * 2 + r) * 64 + lane];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[r][e] += v[e];
+                }
+            }
+            finish(q, s[0], s[1]);
+        }
+        __syncthreads();  // before the next pass's loads
+    }
+}
+
+template <typename XT, bool FP8, int RING, int WK, int WR, int NR>
+__global__ __launch_bounds__(WK * WR * 64) void moe_gate_up(
     const XT* __restrict__ x, int64_t T, int d, const int32_t* __restrict__ ids, int npairs, int k,
     const uint8_t* __restrict__ gate_up, const float* __restrict__ scales, int E, int I,
     int by_pair, typename HType<XT, FP8>::type* __restrict__ H, int parts) {
     extern __shared__ uint16_t list[];
-    __shared__ f32x4_t red[kWaves * 2 * kMaxNT * 64];
-    __shared__ int cnt[kWaves];
+    constexpr int W = WK * WR;
+    constexpr int MT = max_tiles<RING, FP8, 2 * NR, 1>();
+    __shared__ __align__(1024) char rings[W * RING];
+    __shared__ int cnt[W];
     int e;
-    const int m = expert_pairs(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
+    const int m = expert_pairs<W>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
     if (m == 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr = wave / WK, wk = wave - wr * WK;
     constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
     const uint8_t* gu = gate_up + (int64_t)e * 2 * I * d * WB;
     const float* gs = FP8 ? scales + (int64_t)e * 2 * ((I + 127) / 128) * ((d + 127) / 128) : nullptr;
-    const int n0 = blockIdx.x * 16;
+    const int n0 = (blockIdx.x * WR + wr) * 16 * NR;
     const int64_t plane = (int64_t)npairs * I;
-    for (int c = 0; c < m; c += 16 * kMaxNT) {
-        const int mc = min(m - c, 16 * kMaxNT);
-        const int64_t xb = T * d * (int64_t)sizeof(XT);
+    char* const ring = rings + wave * RING;
+    f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings + wr * WK * RING);
+    const int64_t xb = T * d * (int64_t)sizeof(XT);
+    for (int c = 0; c < m; c += 16 * MT) {
+        const int mc = min(m - c, 16 * MT);
         if (mc <= 16)
-            gate_up_pass<XT, FP8, 1, U>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, red);
-        else if (mc <= 32)
-            gate_up_pass<XT, FP8, 2, U / 2>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, red);
+            gate_up_pass<XT, FP8, RING, WK, NR, 1>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, wk, ring, red);
+        else if (MT < 4 || mc <= 32)
+            gate_up_pass<XT, FP8, RING, WK, NR, (MT < 2 ? MT : 2)>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, wk, ring, red);
         else
-            gate_up_pass<XT, FP8, 4, U / 4>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, red);
+            gate_up_pass<XT, FP8, RING, WK, NR, MT>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, wk, ring, red);
     }
 }
 
 // ---- down -----------------------------------------------------------------------------------
-// Work-group: 32 rows of one expert's down matrix (32 columns of y) -> z[pair][d] float32.
-constexpr int kDownTiles = 2;
+// Work-group: WR groups of 16 RT rows of one expert's down matrix (columns of y), K split over WK
+// waves -> z[pair][d] float32.
 
 // factor of part p of h in the sum (half: see kHalfDown)
 template <typename HT>
@@ -354,34 +492,39 @@ __device__ __forceinline__ float part_factor<f16_t>(int p) {
     return p == 0 ? kHalfUp : kHalfUp / 2048.0f;
 }
 
-template <typename HT, bool FP8, int PARTS, int NT, int U>
-__device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int npairs, int d,
-                                          const uint8_t* dn, const float* dns, int I, int c0,
-                                          const uint16_t* list, int m, float* z, f32x4_t* red) {
-    constexpr int RT = kDownTiles;
+template <typename HT, bool FP8, int PARTS, int RING, int WK, int RT, int NT>
+__device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int d, const uint8_t* dn,
+                                          const float* dns, int I, int c0, const uint16_t* list,
+                                          int m, float* z, int wk, char* ring, f32x4_t* red) {
     constexpr int WB = FP8 ? 1 : (int)sizeof(HT);
     const int lane = threadIdx.x & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = lane & 15, g = lane >> 4;
+    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
     const int rb = I * WB;
     const auto wr = make_rsrc(dn, (int64_t)d * rb);
     const int hb = I * (int)sizeof(HT);
     const auto hr = make_rsrc(H, (int64_t)PARTS * plane * sizeof(HT));
     const int pl = (int)(plane * sizeof(HT));
-    int woff[RT], xoff[NT];
+    int woff[RT][2], xoff[NT][2];
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-        woff[r] = c0 + 16 * r + row < d ? (c0 + 16 * r + row) * rb : kOOB;
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-        xoff[n] = 16 * n + row < m ? (int)list[16 * n + row] * hb : kOOB;
+        for (int r = 0; r < RT; ++r) {
+            const int c = c0 + 16 * r + 8 * h + lr;
+            woff[r][h] = c < d ? c * rb : kOOB;
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int t = 16 * n + 8 * h + lr;
+            xoff[n][h] = t < m ? (int)list[t] * hb : kOOB;
+        }
+    }
     const int nl = (rb + kLine - 1) / kLine;
     const float* sc[RT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
         sc[r] = FP8 ? dns + (int64_t)(min(c0 + 16 * r, d - 1) / 128) * nl : nullptr;
     int l0, l1;
-    wave_lines(nl, wave, l0, l1);
+    wave_lines<WK>(nl, wk, l0, l1);
     f32x4_t acc[RT][NT];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -389,6 +532,7 @@ __device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int npairs
         for (int n = 0; n < NT; ++n) acc[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     if constexpr (std::is_same<HT, f16_t>::value) {
         // parts of different weight: one product each
+        constexpr int D = ring_depth<RING, FP8, RT, NT, 1>();
 #pragma unroll
         for (int p = PARTS - 1; p >= 0; --p) {
             f32x4_t t[RT][NT];
@@ -396,67 +540,64 @@ __device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int npairs
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int n = 0; n < NT; ++n) t[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-            int xp[NT];
+            int xp[NT][2];
 #pragma unroll
-            for (int n = 0; n < NT; ++n) xp[n] = xoff[n] >= 0 ? xoff[n] + p * pl : kOOB;
-            lines<HT, FP8, RT, NT, 1, U>(t, wr, woff, rb, hr, xp, hb, 0, sc, l0, l1);
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) xp[n][h] = xoff[n][h] >= 0 ? xoff[n][h] + p * pl : kOOB;
+            lines<HT, FP8, RT, NT, 1, D, 0>(t, wr, woff, rb, hr, xp, hb, 0, sc, l0, l1, ring);
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        acc[r][n][i] = fmaf(part_factor<HT>(p), t[r][n][i], acc[r][n][i]);
+                    for (int e = 0; e < 4; ++e)
+                        acc[r][n][e] = fmaf(part_factor<HT>(p), t[r][n][e], acc[r][n][e]);
         }
     } else {
-        lines<HT, FP8, RT, NT, PARTS, U>(acc, wr, woff, rb, hr, xoff, hb, pl, sc, l0, l1);
+        constexpr int D = ring_depth<RING, FP8, RT, NT, PARTS>();
+        lines<HT, FP8, RT, NT, PARTS, D, kNonTemporal>(acc, wr, woff, rb, hr, xoff, hb, pl, sc, l0,
+                                                       l1, ring);
     }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int n = 0; n < NT; ++n) red[((wave * RT + r) * NT + n) * 64 + lane] = acc[r][n];
-    __syncthreads();
-    for (int q = wave; q < RT * NT; q += kWaves) {
+    join_waves<WK, RT * NT>(&acc[0][0], red, wk, lane, [&](int q, const f32x4_t& s) {
         const int r = q / NT, n = q - r * NT;
-        f32x4_t s = red[q * 64 + lane];
-#pragma unroll
-        for (int w = 1; w < kWaves; ++w) {
-            const f32x4_t v = red[(w * RT * NT + q) * 64 + lane];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[i] += v[i];
-        }
         const int c = c0 + 16 * r + 4 * g;
         // d is a multiple of 4: a lane's four columns are all in or all out
         if (16 * n + row < m && c < d)
             *reinterpret_cast<f32x4_t*>(z + (int64_t)list[16 * n + row] * d + c) = s;
-    }
+    });
 }
 
-template <typename HT, bool FP8, int PARTS, int U>
-__global__ __launch_bounds__(kWaves * 64) void moe_down(
+template <typename HT, bool FP8, int PARTS, int RING, int WK, int WR, int RT>
+__global__ __launch_bounds__(WK * WR * 64) void moe_down(
     const HT* __restrict__ H, int d, const int32_t* __restrict__ ids, int npairs,
     const uint8_t* __restrict__ down, const float* __restrict__ scales, int E, int I, int by_pair,
     float* __restrict__ z) {
     extern __shared__ uint16_t list[];
-    __shared__ f32x4_t red[kWaves * kDownTiles * kMaxNT * 64];
-    __shared__ int cnt[kWaves];
+    constexpr int W = WK * WR;
+    constexpr int MT = max_tiles<RING, FP8, RT, std::is_same<HT, f16_t>::value ? 1 : PARTS>();
+    __shared__ __align__(1024) char rings[W * RING];
+    __shared__ int cnt[W];
     int e;
-    const int m = expert_pairs(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
+    const int m = expert_pairs<W>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
     if (m == 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wr = wave / WK, wk = wave - wr * WK;
     constexpr int WB = FP8 ? 1 : (int)sizeof(HT);
     const uint8_t* dn = down + (int64_t)e * d * I * WB;
     const float* ds = FP8 ? scales + (int64_t)e * ((d + 127) / 128) * ((I + 127) / 128) : nullptr;
-    const int c0 = blockIdx.x * 16 * kDownTiles;
+    const int c0 = (blockIdx.x * WR + wr) * 16 * RT;
     const int64_t plane = (int64_t)npairs * I;
-    for (int c = 0; c < m; c += 16 * kMaxNT) {
-        const int mc = min(m - c, 16 * kMaxNT);
+    char* const ring = rings + wave * RING;
+    f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings + wr * WK * RING);
+    for (int c = 0; c < m; c += 16 * MT) {
+        const int mc = min(m - c, 16 * MT);
         if (mc <= 16)
-            down_pass<HT, FP8, PARTS, 1, U>(H, plane, npairs, d, dn, ds, I, c0, list + c, mc, z, red);
-        else if (mc <= 32)
-            down_pass<HT, FP8, PARTS, 2, U / 2>(H, plane, npairs, d, dn, ds, I, c0, list + c, mc, z, red);
+            down_pass<HT, FP8, PARTS, RING, WK, RT, 1>(H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
+        else if (MT < 4 || mc <= 32)
+            down_pass<HT, FP8, PARTS, RING, WK, RT, (MT < 2 ? MT : 2)>(H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
         else
-            down_pass<HT, FP8, PARTS, 4, U / 4>(H, plane, npairs, d, dn, ds, I, c0, list + c, mc, z, red);
+            down_pass<HT, FP8, PARTS, RING, WK, RT, MT>(H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
     }
 }
 
@@ -496,6 +637,71 @@ __global__ __launch_bounds__(256) void moe_sum(const float* __restrict__ z,
     put4(y + t * d + c, s);
 }
 
+// ---- one token: down and the weighted sum in one kernel ---------------------------------------
+// Work-group: 16 rows of every chosen expert's down matrix (16 columns of y). A wave takes an
+// expert, or one of kc runs of K of it where there are fewer experts than waves; the waves' sums
+// are weighted and added in order, and y is written at once.
+constexpr int kOneWaves = 8;
+
+template <typename HT, bool FP8, int PARTS, int RING, typename YT>
+__global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
+    const HT* __restrict__ H, int d, const int32_t* __restrict__ ids,
+    const float* __restrict__ weights, int k, int kc, const uint8_t* __restrict__ down,
+    const float* __restrict__ scales, int E, int I, YT* __restrict__ y) {
+    constexpr int LP = std::is_same<HT, f16_t>::value ? 1 : PARTS;  // parts of one product
+    constexpr int D = ring_depth<RING, FP8, 1, 1, LP>();
+    __shared__ __align__(1024) char rings[kOneWaves * RING];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
+    const int c0 = blockIdx.x * 16;
+    constexpr int WB = FP8 ? 1 : (int)sizeof(HT);
+    const int rb = I * WB, hb = I * (int)sizeof(HT);
+    const int64_t plane = (int64_t)k * I;
+    const auto hr = make_rsrc(H, (int64_t)PARTS * plane * sizeof(HT));
+    const int pl = (int)(plane * sizeof(HT));
+    const int nl = (rb + kLine - 1) / kLine, per = (nl + kc - 1) / kc;
+    const int woff[1][2] = {{c0 + lr < d ? (c0 + lr) * rb : kOOB,
+                             c0 + 8 + lr < d ? (c0 + 8 + lr) * rb : kOOB}};
+    f32x4_t tot = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int u = wave; u < k * kc; u += kOneWaves) {
+        const int r = u / kc, q = u - r * kc;
+        const int e = __builtin_amdgcn_readfirstlane(ids[r]);
+        if ((unsigned)e >= (unsigned)E) continue;
+        const auto wr = make_rsrc(down + (int64_t)e * d * rb, (int64_t)d * rb);
+        const float* sc[1] = {FP8 ? scales + ((int64_t)e * ((d + 127) / 128) + c0 / 128) * nl
+                                  : nullptr};
+        const int l0 = min(nl, q * per), l1 = min(nl, l0 + per);
+        const float f = weights[r];
+#pragma unroll
+        for (int p = PARTS / LP - 1; p >= 0; --p) {
+            f32x4_t acc[1][1] = {{f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}}};
+            const int xoff[1][2] = {{lr == 0 ? r * hb + p * pl : kOOB, kOOB}};
+            lines<HT, FP8, 1, 1, LP, D, kNonTemporal>(acc, wr, woff, rb, hr, xoff, hb, pl, sc, l0, l1,
+                                                      rings + wave * RING);
+            const float fp = LP == PARTS ? f : f * part_factor<HT>(p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) tot[i] = fmaf(fp, acc[0][0][i], tot[i]);
+        }
+    }
+    f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings);
+    __syncthreads();  // the rings are done with
+    if (row == 0) red[wave * 4 + g] = tot;
+    __syncthreads();
+    // lane g of wave 0: columns 4 g .. (d is a multiple of 4)
+    if (threadIdx.x < 4 && c0 + 4 * (int)threadIdx.x < d) {
+        f32x4_t s = red[threadIdx.x];
+#pragma unroll
+        for (int w = 1; w < kOneWaves; ++w) {
+            const f32x4_t v = red[w * 4 + threadIdx.x];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[i] += v[i];
+        }
+        const float o[4] = {s[0], s[1], s[2], s[3]};
+        put4(y + c0 + 4 * threadIdx.x, o);
+    }
+}
+
 struct Plan {
     int64_t pairs;
     int parts, hbytes;  // parts of h and bytes of an element of one
@@ -527,10 +733,22 @@ struct Args {
     const uint8_t* down;
     const float* dns;
     int64_t E, I;
+    void* y;
+    int ydt;
     void* ws;
     Plan p;
     hipStream_t s;
 };
+
+template <typename YT>
+void sum(const Args& a, YT* y) {
+    const float* z = reinterpret_cast<const float*>(static_cast<char*>(a.ws) + a.p.off_z);
+    moe_sum<YT><<<dim3((unsigned)((a.d + 1023) / 1024), (unsigned)a.T), 256, 0, a.s>>>(
+        z, a.ids, a.w, (int)a.k, (int)a.E, (int)a.d, y);
+}
+
+// lines of a weight row from which it counts as long
+constexpr int kLongRow = 64;
 
 template <typename XT, bool FP8, int PARTS>
 void experts(const Args& a) {
@@ -543,21 +761,47 @@ void experts(const Args& a) {
     const int by_pair = np <= a.E;
     const unsigned slots = (unsigned)(by_pair ? np : a.E);
     const size_t lds = ((size_t)np * sizeof(uint16_t) + 15) / 16 * 16;
-    constexpr int U = 4;
-    moe_gate_up<XT, FP8, U><<<dim3((unsigned)((a.I + 15) / 16), slots), kWaves * 64, lds, a.s>>>(
-        static_cast<const XT*>(a.x), a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus,
-        (int)a.E, (int)a.I, by_pair, H, a.p.parts);
-    constexpr int rows = 16 * kDownTiles;
-    moe_down<HT, FP8, PARTS, U>
-        <<<dim3((unsigned)((a.d + rows - 1) / rows), slots), kWaves * 64, lds, a.s>>>(
-            H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
-}
-
-template <typename YT>
-void sum(const Args& a, void* y) {
-    const float* z = reinterpret_cast<const float*>(static_cast<char*>(a.ws) + a.p.off_z);
-    moe_sum<YT><<<dim3((unsigned)((a.d + 1023) / 1024), (unsigned)a.T), 256, 0, a.s>>>(
-        z, a.ids, a.w, (int)a.k, (int)a.E, (int)a.d, static_cast<YT*>(y));
+    const int gl = (int)((a.d * (FP8 ? 1 : (int)sizeof(XT)) + kLine - 1) / kLine);
+    const int dl = (int)((a.I * (FP8 ? 1 : (int)sizeof(HT)) + kLine - 1) / kLine);
+    const XT* x = static_cast<const XT*>(a.x);
+    // Long rows: more waves along K, so that fewer work-groups take more of a row at a time
+    if (gl >= kLongRow)
+        moe_gate_up<XT, FP8, 16 * 1024, 4, 1, 1>
+            <<<dim3((unsigned)((a.I + 15) / 16), slots), 256, lds, a.s>>>(
+                x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
+                H, a.p.parts);
+    else
+        moe_gate_up<XT, FP8, 24 * 1024, 2, 1, 1>
+            <<<dim3((unsigned)((a.I + 15) / 16), slots), 128, lds, a.s>>>(
+                x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
+                H, a.p.parts);
+    if (a.T == 1) {
+        // one token: as many runs of K as keep the waves busy
+        const int kc = a.k >= kOneWaves ? 1 : (int)(kOneWaves / a.k);
+        const dim3 grid((unsigned)((a.d + 15) / 16));
+        auto one = [&](auto* y) {
+            typedef typename std::remove_pointer<decltype(y)>::type YT;
+            moe_down_one<HT, FP8, PARTS, 18 * 1024, YT><<<grid, kOneWaves * 64, 0, a.s>>>(
+                H, (int)a.d, a.ids, a.w, (int)a.k, kc, a.down, a.dns, (int)a.E, (int)a.I, y);
+        };
+        if (a.ydt == 0)
+            one(static_cast<float*>(a.y));
+        else if constexpr (sizeof(XT) == 2)
+            one(static_cast<XT*>(a.y));
+        return;
+    }
+    if (dl >= kLongRow)
+        moe_down<HT, FP8, PARTS, 24 * 1024, 2, 2, 2>
+            <<<dim3((unsigned)((a.d + 63) / 64), slots), 256, lds, a.s>>>(
+                H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
+    else
+        moe_down<HT, FP8, PARTS, 24 * 1024, 1, 2, 2>
+            <<<dim3((unsigned)((a.d + 63) / 64), slots), 128, lds, a.s>>>(
+                H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
+    if (a.ydt == 0)
+        sum(a, static_cast<float*>(a.y));
+    else if constexpr (sizeof(XT) == 2)
+        sum(a, static_cast<XT*>(a.y));
 }
 
 }  // namespace
@@ -579,7 +823,7 @@ hipError_t launch_moe(const void* x, int xdt, int64_t T, int64_t d, const int32_
                       const void* down, const float* dns, int64_t E, int64_t I, int wdt, void* y,
                       int ydt, void* ws, hipStream_t s) {
     const Args a{x, T, d, ids, w, k, static_cast<const uint8_t*>(gate_up), gus,
-                 static_cast<const uint8_t*>(down), dns, E, I, ws,
+                 static_cast<const uint8_t*>(down), dns, E, I, y, ydt, ws,
                  moe_plan(T, k, d, I, xdt, wdt, ydt), s};
     const bool three = a.p.parts == 3;
     if (wdt == 0)
@@ -592,12 +836,6 @@ hipError_t launch_moe(const void* x, int xdt, int64_t T, int64_t d, const int32_
         three ? experts<bf16_t, true, 3>(a) : experts<bf16_t, true, 2>(a);
     else
         three ? experts<f16_t, true, 3>(a) : experts<f16_t, true, 2>(a);
-    if (ydt == 0)
-        sum<float>(a, y);
-    else if (ydt == 1)
-        sum<bf16_t>(a, y);
-    else
-        sum<f16_t>(a, y);
     return hipGetLastError();
 }
 

@@ -25,44 +25,45 @@ namespace {
 // operands of one K step: 16 bytes of a weight row a lane (four lanes a row: 32 values of 16-bit
 // data, 16 of float32), and the same columns of a token
 template <typename XT, typename WT>
-struct Step;
+struct Step {  // a float32 router over 16-bit activations
+    static constexpr int K = 16;
+    V16 w, x;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t wr, int wo,
+                                         __amdgpu_buffer_rsrc_t xr, int xo) {
+        w = bload16(wr, wo);
+        const auto v = __builtin_amdgcn_raw_buffer_load_b64(xr, xo, 0, 0);
+        x = V16{{(uint32_t)v[0], (uint32_t)v[1], 0u, 0u}};
+    }
+    __device__ __forceinline__ f32x4_t mma() const {
+        float f[8];
+        Elem<XT>::unpack(x, f);
+        f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]), f[e], z, 0, 0, 0);
+        return z;
+    }
+};
 template <typename T>
 struct Step<T, T> {
     static constexpr int K = 4 * Elem<T>::V;
-    __device__ __forceinline__ static f32x4_t mma(__amdgpu_buffer_rsrc_t w, int wo,
-                                                  __amdgpu_buffer_rsrc_t x, int xo) {
-        const f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
-        return Mfma<T>::mma(Mfma<T>::vec(bload16(w, wo)), Mfma<T>::vec(bload16(x, xo)), z);
+    V16 w, x;
+    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t wr, int wo,
+                                         __amdgpu_buffer_rsrc_t xr, int xo) {
+        w = bload16(wr, wo);
+        x = bload16(xr, xo);
     }
-};
-__device__ __forceinline__ f32x4_t mma_f32(const V16& a, const float* b) {
-    f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+    __device__ __forceinline__ f32x4_t mma() const {
+        f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
+        if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-        z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(a.w[e]), b[e], z, 0, 0, 0);
-    return z;
-}
-template <>
-struct Step<float, float> {
-    static constexpr int K = 16;
-    __device__ __forceinline__ static f32x4_t mma(__amdgpu_buffer_rsrc_t w, int wo,
-                                                  __amdgpu_buffer_rsrc_t x, int xo) {
-        float f[4];
-        Elem<float>::unpack(bload16(x, xo), f);
-        return mma_f32(bload16(w, wo), f);
-    }
-};
-// a float32 router over 16-bit activations
-template <typename XT>
-struct Step<XT, float> {
-    static constexpr int K = 16;
-    __device__ __forceinline__ static f32x4_t mma(__amdgpu_buffer_rsrc_t w, int wo,
-                                                  __amdgpu_buffer_rsrc_t x, int xo) {
-        const auto v = __builtin_amdgcn_raw_buffer_load_b64(x, xo, 0, 0);
-        V16 t{{(uint32_t)v[0], (uint32_t)v[1], 0u, 0u}};
-        float f[8];
-        Elem<XT>::unpack(t, f);
-        return mma_f32(bload16(w, wo), f);
+            for (int e = 0; e < 4; ++e)
+                z = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(w.w[e]),
+                                                         __uint_as_float(x.w[e]), z, 0, 0, 0);
+        } else {
+            z = Mfma<T>::mma(Mfma<T>::vec(w), Mfma<T>::vec(x), z);
+        }
+        return z;
     }
 };
 
@@ -83,14 +84,24 @@ __global__ __launch_bounds__(kLogitWaves * 64) void route_logits(
     const int k0 = blockIdx.z * kchunk, k1 = min((int)d, k0 + kchunk);
     constexpr int V = S::K / 4;  // values a lane
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
-    for (int k = k0 + wave * S::K; k < k1; k += kLogitWaves * S::K) {
-        const int c = k + V * g;
-        const bool in = c < k1;
-        const int wo = (in & (e0 + row < E)) ? (int)((row * d + c) * sizeof(WT)) : kOOB;
-        const int xo = (in & (t0 + row < T)) ? (int)((row * d + c) * sizeof(XT)) : kOOB;
-        const f32x4_t s = S::mma(wr, wo, xr, xo);
+    // the loads of U steps before the first product: 200 tokens, 256 experts, d = 5120 12.3 us
+    // with one step at a time
+    constexpr int U = 8;
+    for (int k = k0 + wave * S::K; k < k1; k += U * kLogitWaves * S::K) {
+        S step[U];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc[i] += (double)s[i];
+        for (int u = 0; u < U; ++u) {
+            const int c = k + u * kLogitWaves * S::K + V * g;
+            const bool in = c < k1;
+            step[u].load(wr, (in & (e0 + row < E)) ? (int)((row * d + c) * sizeof(WT)) : kOOB, xr,
+                         (in & (t0 + row < T)) ? (int)((row * d + c) * sizeof(XT)) : kOOB);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const f32x4_t s = step[u].mma();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[i] += (double)s[i];
+        }
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) red[wave][row * 16 + 4 * g + i] = acc[i];  // [token][expert]
@@ -130,10 +141,11 @@ __device__ __forceinline__ double group_reduce(double v, double* red) {
     return v;
 }
 
-// One work-group of 1024 threads a token. Thread i < EP owns expert i; an expert's rank is the
-// number of experts before it in the order, counted by 1024 / EP threads an expert from the keys
-// in LDS: E * E / 1024 comparisons a thread and one exchange, where k rounds of a maximum over
-// the work-group would take 10 steps of exchange each.
+// One work-group a token. Thread i < EP owns expert i (EP: E rounded up to a power of two); an
+// expert's rank is the number of experts before it in the order, counted by blockDim / EP threads
+// an expert from the keys in LDS: one exchange, where k rounds of a maximum over the work-group
+// would take several each. Softmax weights that are divided by their chosen sum need no sum over
+// the others: exp(z - top) / sum of the chosen, with the scores of k experts only.
 __global__ __launch_bounds__(1024) void route_choose(
     const double* __restrict__ part, int KS, int T, int E, int EP, const float* __restrict__ bias,
     int k, int sigmoid, int renorm, float scale, const int32_t* __restrict__ n_valid,
@@ -141,7 +153,7 @@ __global__ __launch_bounds__(1024) void route_choose(
     __shared__ uint64_t keys[1024];
     __shared__ int rank[1024];
     __shared__ double red[16];
-    __shared__ double chosen[64];
+    __shared__ double chosen[32];
     const int t = blockIdx.x, i = threadIdx.x;
     if (n_valid && t >= *n_valid) {
         if (i < k) {
@@ -154,26 +166,29 @@ __global__ __launch_bounds__(1024) void route_choose(
     double z = 0.0;
     if (mine)
         for (int s = 0; s < KS; ++s) z += part[((int64_t)s * T + t) * E + i];
-    double p;
+    // the score of a softmax by its logit alone, until the chosen are known
+    const bool late = !sigmoid && renorm && !bias;
+    double p = z;
     if (sigmoid) {
         p = 1.0 / (1.0 + exp(-z));
-    } else {
+    } else if (!late) {
         const double top = group_reduce<true>(mine ? z : -HUGE_VAL, red);
         p = mine ? exp(z - top) : 0.0;
         p /= group_reduce<false>(p, red);
     }
-    uint64_t key = 0u;  // below every expert's
-    if (mine) key = key_of(bias ? p + (double)bias[i] : z);
-    keys[i] = key;
-    rank[i] = 0;
-    __syncthreads();
-    // thread i counts for expert i % EP over the 1024 / EP-th part of the experts
+    if (i < EP) {
+        keys[i] = mine ? key_of(bias ? p + (double)bias[i] : z) : 0u;  // 0: below every expert's
+        rank[i] = 0;
+    }
+    const bool nan = __syncthreads_or(mine && !(z == z));
+    // thread i counts for expert i % EP over the i / EP-th part of the experts
     const int me = i & (EP - 1);
     if (me < E) {
-        const int parts = 1024 / EP, per = (E + parts - 1) / parts;
+        const int parts = (int)blockDim.x / EP, per = (E + parts - 1) / parts;
         const int lo = min(E, (i / EP) * per), hi = min(E, lo + per);
         const uint64_t m = keys[me];
         int n = 0;
+#pragma unroll 8
         for (int j = lo; j < hi; ++j) n += keys[j] > m - (uint64_t)(j < me);
         if (n) atomicAdd(&rank[me], n);  // whole numbers: the order of the additions is free
     }
@@ -184,15 +199,22 @@ __global__ __launch_bounds__(1024) void route_choose(
         ids[(int64_t)t * k + r] = i;
     }
     __syncthreads();
-    if (r < k) {
-        double w = p;
-        if (renorm) {
-            double sum = 0.0;
-            for (int j = 0; j < k; ++j) sum += chosen[j];
-            w = sum > 0.0 || !(sum == sum) ? p / sum : 0.0;
-        }
-        weights[(int64_t)t * k + r] = (float)(w * (double)scale);
+    if (late) {
+        // (a NaN logit makes every score NaN, as in the softmax over all experts)
+        const double top = chosen[0];
+        const double e = i < k ? (nan ? __longlong_as_double(0x7ff8000000000000ll)
+                                      : exp(chosen[i] - top))
+                               : 0.0;
+        __syncthreads();
+        if (i < k) chosen[i] = e;
+        __syncthreads();
     }
+    if (i >= k) return;  // thread i: the expert of rank i
+    double w = chosen[i], sum = 0.0;
+    if (renorm)
+        for (int j = 0; j < k; ++j) sum += chosen[j];
+    if (renorm) w = sum > 0.0 || !(sum == sum) ? w / sum : 0.0;
+    weights[(int64_t)t * k + i] = (float)(w * (double)scale);
 }
 
 template <typename XT, typename WT>
@@ -240,7 +262,8 @@ hipError_t launch_route(const void* x, int xdt, int64_t T, int64_t d, const void
         logits<f16_t, float>(x, w, T, E, d, kchunk, KS, part, s);
     int EP = 64;
     while (EP < E) EP *= 2;
-    route_choose<<<dim3((unsigned)T), 1024, 0, s>>>(part, KS, (int)T, (int)E, EP, bias, (int)k,
+    const int threads = EP <= 128 ? 512 : 1024;
+    route_choose<<<dim3((unsigned)T), threads, 0, s>>>(part, KS, (int)T, (int)E, EP, bias, (int)k,
                                                    sigmoid, renorm, scale, n_valid, ids, weights);
     return hipGetLastError();
 }
