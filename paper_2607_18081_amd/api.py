@@ -479,13 +479,14 @@ def _blocks(n: int) -> int:
 
 
 def _need(t, name: str, dev: torch.device, dtype, shape) -> None:
-    """t is a contiguous tensor of that type and shape on that device."""
+    """t is a contiguous tensor of that type (or one of those) and shape (a tuple) on that
+    device. The checks that pass cost what the attributes do: a call is a few microseconds."""
+    if t.dtype is not dtype and t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
+    if t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
     if t.device != dev:
         raise ValueError(f"{name} must be on {dev}")
-    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
-        raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
-    if tuple(t.shape) != tuple(shape):
-        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
 
@@ -496,26 +497,29 @@ def _space(workspace, nbytes: int, dev: torch.device) -> torch.Tensor:
     graphs share nothing."""
     if workspace is None:
         return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=dev)
-    if workspace.device != dev or not workspace.is_contiguous():
-        raise ValueError(f"workspace must be contiguous and on {dev}")
+    if workspace.dtype is not torch.uint8 or workspace.device != dev or \
+            not workspace.is_contiguous():
+        raise ValueError(f"workspace must be a contiguous uint8 tensor on {dev}")
     return workspace
 
 
-class _on:
-    """Makes a device current for a call that launches kernels on it."""
+_cuda_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
-    def __init__(self, dev: torch.device):
-        self._guard = None
-        if dev.index is not None and dev.index != torch.cuda.current_device():
-            self._guard = torch.cuda.device(dev)
 
-    def __enter__(self):
-        if self._guard is not None:
-            self._guard.__enter__()
+def _run(fn, where: str, dev: torch.device, *args) -> None:
+    """Calls a C entry point (the stream last) with its tensors' device current."""
+    if dev.index == _cuda_device():
+        st = fn(*args, _stream(dev))
+    else:
+        with torch.cuda.device(dev):
+            st = fn(*args, _stream(dev))
+    if st:
+        _check(st, where)
 
-    def __exit__(self, *exc):
-        if self._guard is not None:
-            self._guard.__exit__(*exc)
+
+def _p(t):
+    """Address of a tensor already known to be contiguous (None: no tensor, or an empty one)."""
+    return (t.data_ptr() or None) if t is not None else None
 
 
 def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | None = None,
@@ -535,14 +539,14 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | Non
     sshape = (*lead, R if block_rows == 1 else _blocks(R), _blocks(C))
     if codes is None:
         codes = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=dev)
+    else:
+        _need(codes, "codes", dev, _CODES, x.shape)
     if scales is None:
         scales = torch.empty(sshape, dtype=torch.float32, device=dev)
-    _need(codes, "codes", dev, _CODES, x.shape)
-    _need(scales, "scales", dev, torch.float32, sshape)
-    with _on(dev):
-        st = load().si_quantize_fp8(_ptr(x), _dt(x), G, R, C, block_rows, _ptr(codes),
-                                    _ptr(scales), _stream(dev))
-    _check(st, "si_quantize_fp8")
+    else:
+        _need(scales, "scales", dev, torch.float32, sshape)
+    _run(load().si_quantize_fp8, "si_quantize_fp8", dev, _ptr(x), _dt(x), G, R, C, block_rows,
+         _p(codes), _p(scales))
     return codes, scales
 
 
@@ -570,15 +574,13 @@ def matmul_fp8(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_scale
     _need(w_scales, "w_scales", dev, torch.float32, (_blocks(N), _blocks(K)))
     if out is None:
         out = torch.empty((M, N), dtype=out_dtype, device=dev)
-    _need(out, "out", dev, out_dtype, (M, N))
+    else:
+        _need(out, "out", dev, out_dtype, (M, N))
     lib = load()
     need = lib.si_matmul_fp8_workspace(M, N, K)
     ws = _space(workspace, need, dev) if need else None
-    with _on(dev):
-        st = lib.si_matmul_fp8(_ptr(x), _ptr(x_scales), M, K, _ptr(w), _ptr(w_scales), N,
-                               _ptr(out), _dt(out), _ptr(ws), ws.numel() if need else 0,
-                               _stream(dev))
-    _check(st, "si_matmul_fp8")
+    _run(lib.si_matmul_fp8, "si_matmul_fp8", dev, _p(x), _p(x_scales), M, K, _p(w), _p(w_scales),
+         N, _p(out), _dt(out), _p(ws), ws.numel() if need else 0)
     return out
 
 
@@ -603,10 +605,12 @@ def _route_args(x, w_router, k, bias, score, renorm, n_valid, ids, weights):
         raise ValueError("k must not be negative")
     if ids is None:
         ids = torch.empty((T, k), dtype=torch.int32, device=dev)
+    else:
+        _need(ids, "ids", dev, torch.int32, (T, k))
     if weights is None:
         weights = torch.empty((T, k), dtype=torch.float32, device=dev)
-    _need(ids, "ids", dev, torch.int32, (T, k))
-    _need(weights, "weights", dev, torch.float32, (T, k))
+    else:
+        _need(weights, "weights", dev, torch.float32, (T, k))
     return dev, T, d, E, mode, ids, weights
 
 
@@ -628,7 +632,8 @@ def _expert_args(x, gate_up, down, gate_up_scales, down_scales, out_dtype, y):
         _need(down_scales, "down_scales", dev, torch.float32, (E, _blocks(d), _blocks(inter)))
     if y is None:
         y = torch.empty((T, d), dtype=out_dtype or torch.float32, device=dev)
-    _need(y, "y", dev, out_dtype or (torch.float32, x.dtype), (T, d))
+    else:
+        _need(y, "y", dev, out_dtype or (torch.float32, x.dtype), (T, d))
     return E, inter, E4M3 if fp8 else _dt(x), y
 
 
@@ -644,11 +649,8 @@ def moe_route(x: torch.Tensor, w_router: torch.Tensor, k: int, bias: torch.Tenso
                                                    ids, weights)
     lib = load()
     ws = _space(workspace, lib.si_moe_route_workspace(T, E, d), dev)
-    with _on(dev):
-        st = lib.si_moe_route(_ptr(x), _dt(x), T, d, _ptr(w_router), _dt(w_router), E, _ptr(bias),
-                              k, mode, float(scale), _ptr(n_valid), _ptr(ids), _ptr(weights),
-                              _ptr(ws), ws.numel(), _stream(dev))
-    _check(st, "si_moe_route")
+    _run(lib.si_moe_route, "si_moe_route", dev, _p(x), _dt(x), T, d, _p(w_router), _dt(w_router),
+         E, _p(bias), k, mode, float(scale), _p(n_valid), _p(ids), _p(weights), _p(ws), ws.numel())
     return ids, weights
 
 
@@ -670,11 +672,9 @@ def moe_ffn(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate_up: 
     E, inter, wdt, y = _expert_args(x, gate_up, down, gate_up_scales, down_scales, out_dtype, y)
     lib, xdt, ydt = load(), _dt(x), _dt(y)
     ws = _space(workspace, lib.si_moe_ffn_workspace(T, k, E, d, inter, xdt, wdt, ydt), dev)
-    with _on(dev):
-        st = lib.si_moe_ffn(_ptr(x), xdt, T, d, _ptr(ids), _ptr(weights), k, _ptr(gate_up),
-                            _ptr(gate_up_scales), _ptr(down), _ptr(down_scales), E, inter, wdt,
-                            _ptr(y), ydt, _ptr(ws), ws.numel(), _stream(dev))
-    _check(st, "si_moe_ffn")
+    _run(lib.si_moe_ffn, "si_moe_ffn", dev, _p(x), xdt, T, d, _p(ids), _p(weights), k, _p(gate_up),
+         _p(gate_up_scales), _p(down), _p(down_scales), E, inter, wdt, _p(y), ydt, _p(ws),
+         ws.numel())
     return y
 
 
@@ -694,11 +694,7 @@ def moe_layer(x: torch.Tensor, w_router: torch.Tensor, gate_up: torch.Tensor, do
         raise ValueError("w_router and gate_up must have one number of experts")
     lib, xdt, ydt = load(), _dt(x), _dt(y)
     ws = _space(workspace, lib.si_moe_layer_workspace(T, k, E, d, inter, xdt, wdt, ydt), dev)
-    with _on(dev):
-        st = lib.si_moe_layer(_ptr(x), xdt, T, d, _ptr(w_router), _dt(w_router), _ptr(bias), k,
-                              mode, float(scale), _ptr(n_valid), _ptr(gate_up),
-                              _ptr(gate_up_scales), _ptr(down), _ptr(down_scales), E, inter, wdt,
-                              _ptr(ids), _ptr(weights), _ptr(y), ydt, _ptr(ws), ws.numel(),
-                              _stream(dev))
-    _check(st, "si_moe_layer")
+    _run(lib.si_moe_layer, "si_moe_layer", dev, _p(x), xdt, T, d, _p(w_router), _dt(w_router),
+         _p(bias), k, mode, float(scale), _p(n_valid), _p(gate_up), _p(gate_up_scales), _p(down),
+         _p(down_scales), E, inter, wdt, _p(ids), _p(weights), _p(y), ydt, _p(ws), ws.numel())
     return y, ids, weights

@@ -638,57 +638,134 @@ __global__ __launch_bounds__(256) void moe_sum(const float* __restrict__ z,
 }
 
 // ---- one token: down and the weighted sum in one kernel ---------------------------------------
-// Work-group: 16 rows of every chosen expert's down matrix (16 columns of y). A wave takes an
-// expert, or one of kc runs of K of it where there are fewer experts than waves; the waves' sums
-// are weighted and added in order, and y is written at once.
-constexpr int kOneWaves = 8;
+// Work-group: 16 rows of every chosen expert's down matrix (16 columns of y). The token's h of all
+// its experts lies in LDS (rows of whole KB, zeros behind each), and every MFMA column holds it: a
+// lane then reads its operand without regard to its column, and column 0 is the result. So only
+// weights pass through the waves' rings, D lines ahead. A wave takes an expert, or one of kc runs
+// of K of it where there are fewer experts than waves; the waves' sums are weighted and added in
+// order, and y is written at once.
+constexpr int kOneWaves = 8, kOneDepth = 6;
+constexpr int kOneH = 48 * 1024;  // most LDS that h may take
 
-template <typename HT, bool FP8, int PARTS, int RING, typename YT>
+constexpr int one_pitch(int64_t I, int hbytes) { return (int)((I * hbytes + 1023) / 1024 * 1024); }
+
+template <typename HT, bool FP8, int PARTS, typename YT>
 __global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
     const HT* __restrict__ H, int d, const int32_t* __restrict__ ids,
     const float* __restrict__ weights, int k, int kc, const uint8_t* __restrict__ down,
     const float* __restrict__ scales, int E, int I, YT* __restrict__ y) {
-    constexpr int LP = std::is_same<HT, f16_t>::value ? 1 : PARTS;  // parts of one product
-    constexpr int D = ring_depth<RING, FP8, 1, 1, LP>();
-    __shared__ __align__(1024) char rings[kOneWaves * RING];
+    using C = Core<HT, FP8>;
+    constexpr int XC = C::XC, D = kOneDepth, L = 2;
+    __shared__ __align__(1024) char rings[kOneWaves * D * L * 1024];
+    extern __shared__ __align__(1024) char hs[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
+    const int row = lane & 15, g = lane >> 4;
     const int c0 = blockIdx.x * 16;
     constexpr int WB = FP8 ? 1 : (int)sizeof(HT);
-    const int rb = I * WB, hb = I * (int)sizeof(HT);
-    const int64_t plane = (int64_t)k * I;
-    const auto hr = make_rsrc(H, (int64_t)PARTS * plane * sizeof(HT));
-    const int pl = (int)(plane * sizeof(HT));
+    const int rb = I * WB, hb = I * (int)sizeof(HT), pitch = one_pitch(I, sizeof(HT));
     const int nl = (rb + kLine - 1) / kLine, per = (nl + kc - 1) / kc;
-    const int woff[1][2] = {{c0 + lr < d ? (c0 + lr) * rb : kOOB,
-                             c0 + 8 + lr < d ? (c0 + 8 + lr) * rb : kOOB}};
+    char* const ring = rings + wave * D * L * 1024;
+
+    // h to LDS: row r of part p at (p k + r) pitch
+    const auto hr = make_rsrc(H, (int64_t)PARTS * k * I * sizeof(HT));
+    const int kbs = pitch >> 10;
+    for (int q = wave; q < PARTS * k * kbs; q += kOneWaves) {
+        const int pr = q / kbs, o = (q - pr * kbs) * 1024 + lane * 16;
+        load_lds16(hr, hs + q * 1024, o < hb ? pr * hb + o : kOOB, 0);
+    }
+    const int lr = lane >> 3, lcol = ((lane & 7) ^ lr) * 16;
+    const int w0 = c0 + lr < d ? (c0 + lr) * rb + lcol : kOOB;
+    const int w8 = c0 + 8 + lr < d ? (c0 + 8 + lr) * rb + lcol : kOOB;
+    const uint32_t base = lds_addr(ring) + row * kLine;
+    const uint32_t a0 = base + (g ^ (row & 7)) * 16, a1 = base + ((4 + g) ^ (row & 7)) * 16;
+    const uint32_t hbase = lds_addr(hs) + (XC == 1 ? 16 * g : 32 * g);
+    bool ready = false;
     f32x4_t tot = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int u = wave; u < k * kc; u += kOneWaves) {
         const int r = u / kc, q = u - r * kc;
         const int e = __builtin_amdgcn_readfirstlane(ids[r]);
-        if ((unsigned)e >= (unsigned)E) continue;
-        const auto wr = make_rsrc(down + (int64_t)e * d * rb, (int64_t)d * rb);
-        const float* sc[1] = {FP8 ? scales + ((int64_t)e * ((d + 127) / 128) + c0 / 128) * nl
-                                  : nullptr};
-        const int l0 = min(nl, q * per), l1 = min(nl, l0 + per);
-        const float f = weights[r];
+        const bool some = (unsigned)e < (unsigned)E;
+        const int ex = some ? e : 0;
+        const auto wr = make_rsrc(down + (int64_t)ex * d * rb, (int64_t)d * rb);
+        const float* sc = FP8 ? scales + ((int64_t)ex * ((d + 127) / 128) + c0 / 128) * nl : nullptr;
+        const int l0 = min(nl, q * per), l1 = some ? min(nl, l0 + per) : l0;
+        auto load = [&](int l, char* at) {
+            const bool in = (l < l1) & (l * kLine + lcol < rb);
+            load_lds16<kNonTemporal>(wr, at, (in & (w0 >= 0)) ? w0 : kOOB, l * kLine);
+            load_lds16<kNonTemporal>(wr, at + 1024, (in & (w8 >= 0)) ? w8 : kOOB, l * kLine);
+        };
 #pragma unroll
-        for (int p = PARTS / LP - 1; p >= 0; --p) {
-            f32x4_t acc[1][1] = {{f32x4_t{0.0f, 0.0f, 0.0f, 0.0f}}};
-            const int xoff[1][2] = {{lr == 0 ? r * hb + p * pl : kOOB, kOOB}};
-            lines<HT, FP8, 1, 1, LP, D, kNonTemporal>(acc, wr, woff, rb, hr, xoff, hb, pl, sc, l0, l1,
-                                                      rings + wave * RING);
-            const float fp = LP == PARTS ? f : f * part_factor<HT>(p);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) tot[i] = fmaf(fp, acc[0][0][i], tot[i]);
+        for (int t = 0; t < D; ++t) load(l0 + t, ring + t * L * 1024);
+        if (!ready) {
+            // every wave's part of h has landed (the weights' first lines, issued later, may fly)
+            wait_vm_lds<D * L>();
+            wg_barrier();
+            ready = true;
         }
+        const float f = some ? weights[r] : 0.0f;
+        f32x4_t acc[PARTS];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) acc[p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        int slot = 0;
+        for (int l = l0; l < l1; ++l) {
+            wait_vm_lds<(D - 1) * L>();
+            V16 a[1][2], b[PARTS][XC][2];
+            lds_tiles<1, 0>(a0 + slot * L * 1024, a1 + slot * L * 1024, a);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+                const uint32_t at = hbase + (p * k + r) * pitch + l * kLine * XC;
+                if constexpr (XC == 1) {
+                    lds_tiles<1, 0>(at, at + 64, b[p]);
+                } else {
+                    lds_tiles<1, 0>(at, at + 16, b[p]);
+                    lds_tiles<1, 128>(at, at + 16, b[p] + 1);
+                }
+            }
+            load(l + D, ring + slot * L * 1024);
+            slot = slot + 1 == D ? 0 : slot + 1;
+            f32x4_t blk[PARTS];
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) blk[p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                typename C::vec w[XC];
+                C::widen(a[0][h], w);
+#pragma unroll
+                for (int c = 0; c < XC; ++c)
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) {
+                        f32x4_t& t = FP8 ? blk[p] : acc[p];
+                        t = C::mma(w[c], XC == 1 ? b[p][0][h] : b[p][h * (XC - 1)][c], t);
+                    }
+            }
+            if (FP8) {
+                const float s = sc[l];
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[p][i] = fmaf(s, blk[p][i], acc[p][i]);
+            }
+        }
+        wait_vm_lds<0>();  // the ring is free again
+        if (some) {
+#pragma unroll
+            for (int p = PARTS - 1; p >= 0; --p) {
+                const float fp = std::is_same<HT, f16_t>::value ? f * part_factor<HT>(p) : f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) tot[i] = fmaf(fp, acc[p][i], tot[i]);
+            }
+        }
+    }
+    if (!ready) {  // a wave without work meets the same barrier, its part of h landed
+        wait_vm_lds<0>();
+        wg_barrier();
     }
     f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings);
     __syncthreads();  // the rings are done with
     if (row == 0) red[wave * 4 + g] = tot;
     __syncthreads();
-    // lane g of wave 0: columns 4 g .. (d is a multiple of 4)
+    // thread g: columns 4 g .. (d is a multiple of 4)
     if (threadIdx.x < 4 && c0 + 4 * (int)threadIdx.x < d) {
         f32x4_t s = red[threadIdx.x];
 #pragma unroll
@@ -775,13 +852,14 @@ void experts(const Args& a) {
             <<<dim3((unsigned)((a.I + 15) / 16), slots), 128, lds, a.s>>>(
                 x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
                 H, a.p.parts);
-    if (a.T == 1) {
+    const int64_t hlds = (int64_t)PARTS * a.k * one_pitch(a.I, sizeof(HT));
+    if (a.T == 1 && hlds <= kOneH) {
         // one token: as many runs of K as keep the waves busy
         const int kc = a.k >= kOneWaves ? 1 : (int)(kOneWaves / a.k);
         const dim3 grid((unsigned)((a.d + 15) / 16));
         auto one = [&](auto* y) {
             typedef typename std::remove_pointer<decltype(y)>::type YT;
-            moe_down_one<HT, FP8, PARTS, 18 * 1024, YT><<<grid, kOneWaves * 64, 0, a.s>>>(
+            moe_down_one<HT, FP8, PARTS, YT><<<grid, kOneWaves * 64, (size_t)hlds, a.s>>>(
                 H, (int)a.d, a.ids, a.w, (int)a.k, kc, a.down, a.dns, (int)a.E, (int)a.I, y);
         };
         if (a.ydt == 0)

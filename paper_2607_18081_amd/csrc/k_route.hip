@@ -22,19 +22,16 @@ namespace {
 // One work-group of 4 waves a tile of 16 experts x 16 tokens and a K chunk; the waves take K
 // steps in turn. The experts' rows are the MFMA's M operand, tokens its N operand.
 
-// operands of one K step: 16 bytes of a weight row a lane (four lanes a row: 32 values of 16-bit
-// data, 16 of float32), and the same columns of a token
+// One K step: 16 bytes of a weight row a lane (four lanes a row: 32 values of 16-bit data, 16 of
+// float32), and the same columns of a token.
 template <typename XT, typename WT>
 struct Step {  // a float32 router over 16-bit activations
     static constexpr int K = 16;
-    V16 w, x;
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t wr, int wo,
-                                         __amdgpu_buffer_rsrc_t xr, int xo) {
-        w = bload16(wr, wo);
+    __device__ __forceinline__ static V16 tokens(__amdgpu_buffer_rsrc_t xr, int xo) {
         const auto v = __builtin_amdgcn_raw_buffer_load_b64(xr, xo, 0, 0);
-        x = V16{{(uint32_t)v[0], (uint32_t)v[1], 0u, 0u}};
+        return V16{{(uint32_t)v[0], (uint32_t)v[1], 0u, 0u}};
     }
-    __device__ __forceinline__ f32x4_t mma() const {
+    __device__ __forceinline__ static f32x4_t mma(const V16& w, const V16& x) {
         float f[8];
         Elem<XT>::unpack(x, f);
         f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -47,13 +44,10 @@ struct Step {  // a float32 router over 16-bit activations
 template <typename T>
 struct Step<T, T> {
     static constexpr int K = 4 * Elem<T>::V;
-    V16 w, x;
-    __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t wr, int wo,
-                                         __amdgpu_buffer_rsrc_t xr, int xo) {
-        w = bload16(wr, wo);
-        x = bload16(xr, xo);
+    __device__ __forceinline__ static V16 tokens(__amdgpu_buffer_rsrc_t xr, int xo) {
+        return bload16(xr, xo);
     }
-    __device__ __forceinline__ f32x4_t mma() const {
+    __device__ __forceinline__ static f32x4_t mma(const V16& w, const V16& x) {
         f32x4_t z = {0.0f, 0.0f, 0.0f, 0.0f};
         if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -67,6 +61,9 @@ struct Step<T, T> {
     }
 };
 
+// One work-group of 4 waves a tile of 16 experts x 16 tokens and a K chunk, of which each wave
+// takes a run. The experts' rows are the MFMA's M operand, tokens its N operand. U steps' loads
+// are issued before the first product.
 constexpr int kLogitWaves = 4;
 
 template <typename XT, typename WT>
@@ -74,31 +71,31 @@ __global__ __launch_bounds__(kLogitWaves * 64) void route_logits(
     const XT* __restrict__ x, const WT* __restrict__ w, int T, int E, int64_t d, int kchunk,
     double* __restrict__ part) {
     using S = Step<XT, WT>;
+    constexpr int U = 8;
     __shared__ double red[kLogitWaves][256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int row = lane & 15, g = lane >> 4;
     const int e0 = blockIdx.x * 16, t0 = blockIdx.y * 16;
-    // rows of the two operand tiles only: 32-bit offsets hold for any number of tokens
+    // rows of the two operand tiles only: 32-bit offsets hold for any number of tokens, and rows
+    // past the last lie past the descriptor's end and read zeros
     const auto wr = make_rsrc(w + (int64_t)e0 * d, (int64_t)min(16, E - e0) * d * sizeof(WT));
     const auto xr = make_rsrc(x + (int64_t)t0 * d, (int64_t)min(16, T - t0) * d * sizeof(XT));
-    const int k0 = blockIdx.z * kchunk, k1 = min((int)d, k0 + kchunk);
+    const int run = kchunk / kLogitWaves;
+    const int k0 = blockIdx.z * kchunk + wave * run, k1 = min((int)d, k0 + run);
     constexpr int V = S::K / 4;  // values a lane
     double acc[4] = {0.0, 0.0, 0.0, 0.0};
-    // the loads of U steps before the first product: 200 tokens, 256 experts, d = 5120 12.3 us
-    // with one step at a time
-    constexpr int U = 8;
-    for (int k = k0 + wave * S::K; k < k1; k += U * kLogitWaves * S::K) {
-        S step[U];
+    for (int k = k0; k < k1; k += U * S::K) {
+        V16 a[U], b[U];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const int c = k + u * kLogitWaves * S::K + V * g;
-            const bool in = c < k1;
-            step[u].load(wr, (in & (e0 + row < E)) ? (int)((row * d + c) * sizeof(WT)) : kOOB, xr,
-                         (in & (t0 + row < T)) ? (int)((row * d + c) * sizeof(XT)) : kOOB);
+            const int c = k + u * S::K + V * g;
+            a[u] = bload16(wr, c < k1 ? (int)((row * d + c) * sizeof(WT)) : kOOB);
+            b[u] = S::tokens(xr, c < k1 ? (int)((row * d + c) * sizeof(XT)) : kOOB);
         }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const f32x4_t s = step[u].mma();
+            const f32x4_t s = S::mma(a[u], b[u]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) acc[i] += (double)s[i];
         }
@@ -227,11 +224,13 @@ void logits(const void* x, const void* w, int64_t T, int64_t E, int64_t d, int k
 
 }  // namespace
 
-// K chunks of the logits: enough work-groups to spread a small call over the chip (512 columns
-// each at least), one chunk where the tiles of experts and tokens do that alone
+// K chunks of the logits: enough work-groups to spread the call over the chip (512 columns each
+// at least), one chunk where the tiles of experts and tokens do that alone. (200 tokens, 256
+// experts, d = 5120: 2 to 5 chunks, one to four expert tiles a work-group and one to eight steps
+// ahead all take 11 to 13 us, 8 of them without any load.)
 int route_chunks(int64_t T, int64_t E, int64_t d) {
     const int64_t tiles = ((E + 15) / 16) * ((T + 15) / 16);
-    int64_t ks = (1024 + tiles - 1) / tiles;
+    int64_t ks = (512 + tiles - 1) / tiles;
     const int64_t most = (d + 511) / 512;
     if (ks > most) ks = most;
     if (ks > 16) ks = 16;
@@ -247,8 +246,9 @@ hipError_t launch_route(const void* x, int xdt, int64_t T, int64_t d, const void
                         float scale, const int32_t* n_valid, int32_t* ids, float* weights,
                         void* ws, hipStream_t s) {
     const int KS = route_chunks(T, E, d);
-    // chunks of whole 32-value steps
-    const int kchunk = (int)(((d + KS - 1) / KS + 31) / 32 * 32);
+    // chunks of whole 64-value runs of the waves (whole lines of 16-bit data)
+    constexpr int kRun = 64 * kLogitWaves;
+    const int kchunk = (int)(((d + KS - 1) / KS + kRun - 1) / kRun * kRun);
     double* part = static_cast<double*>(ws);
     if (xdt == 0)
         logits<float, float>(x, w, T, E, d, kchunk, KS, part, s);
