@@ -3,6 +3,7 @@
 
 #include "common.h"
 #include "launch.h"
+#include "route.h"
 #include "selectinfer.h"
 
 namespace {
@@ -537,10 +538,11 @@ int si_moe_route(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* 
         return SI_ERR_INVALID;
     if (!ws || ws_bytes < si_moe_route_workspace(T, E, d) || !aligned16(ws))
         return SI_ERR_WORKSPACE;
-    return from_hip(si::launch_route(x, xdt, T, d, w_router, wdt, E, bias, k,
-                                     (mode & SI_ROUTE_SIGMOID) != 0, (mode & SI_ROUTE_RENORM) != 0,
-                                     scale, n_valid, ids, weights, ws,
-                                     static_cast<hipStream_t>(hip_stream)));
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const si::Choice c = si::route_logits_of(x, xdt, T, d, w_router, wdt, E, bias, k,
+                                             (mode & SI_ROUTE_SIGMOID) != 0,
+                                             (mode & SI_ROUTE_RENORM) != 0, scale, n_valid, ws, s);
+    return from_hip(si::launch_choose(c, ids, weights, s));
 }
 
 size_t si_moe_ffn_workspace(int64_t T, int64_t k, int64_t E, int64_t d, int64_t I, si_dtype xdt,
@@ -561,7 +563,9 @@ int si_moe_ffn(const void* x, si_dtype xdt, int64_t T, int64_t d, const int32_t*
         return SI_ERR_INVALID;
     if (!ws || ws_bytes < si_moe_ffn_workspace(T, k, E, d, I, xdt, wdt, ydt) || !aligned16(ws))
         return SI_ERR_WORKSPACE;
-    return from_hip(si::launch_moe(x, xdt, T, d, ids, weights, k, gate_up, gate_up_scales, down,
+    // (only a choice writes ids and weights)
+    return from_hip(si::launch_moe(x, xdt, T, d, const_cast<int32_t*>(ids),
+                                   const_cast<float*>(weights), k, gate_up, gate_up_scales, down,
                                    down_scales, E, I, wdt, y, ydt, ws,
                                    static_cast<hipStream_t>(hip_stream)));
 }
@@ -588,11 +592,17 @@ int si_moe_layer(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* 
     const size_t ffn = round256(si_moe_ffn_workspace(T, k, E, d, I, xdt, wdt, ydt));
     if (!ws || ws_bytes < si_moe_layer_workspace(T, k, E, d, I, xdt, wdt, ydt) || !aligned16(ws))
         return SI_ERR_WORKSPACE;
-    bad = si_moe_route(x, xdt, T, d, w_router, rdt, E, bias, k, mode, scale, n_valid, ids, weights,
-                       static_cast<char*>(ws) + ffn, ws_bytes - ffn, hip_stream);
-    if (bad) return bad;
-    return si_moe_ffn(x, xdt, T, d, ids, weights, k, gate_up, gate_up_scales, down, down_scales, E,
-                      I, wdt, y, ydt, ws, ffn, hip_stream);
+    hipStream_t s = static_cast<hipStream_t>(hip_stream);
+    const si::Choice c = si::route_logits_of(
+        x, xdt, T, d, w_router, rdt, E, bias, k, (mode & SI_ROUTE_SIGMOID) != 0,
+        (mode & SI_ROUTE_RENORM) != 0, scale, n_valid, static_cast<char*>(ws) + ffn, s);
+    const bool later = si::moe_chooses(T, d, E, xdt);
+    if (!later) {
+        const hipError_t e = si::launch_choose(c, ids, weights, s);
+        if (e != hipSuccess) return from_hip(e);
+    }
+    return from_hip(si::launch_moe(x, xdt, T, d, ids, weights, k, gate_up, gate_up_scales, down,
+                                   down_scales, E, I, wdt, y, ydt, ws, s, later ? &c : nullptr));
 }
 
 }  // extern "C"

@@ -23,6 +23,7 @@
 #include "launch.h"
 #include "mfma.h"
 #include "pipe.h"
+#include "route.h"
 
 namespace si {
 
@@ -637,49 +638,208 @@ __global__ __launch_bounds__(256) void moe_sum(const float* __restrict__ z,
     put4(y + t * d + c, s);
 }
 
-// ---- one token: down and the weighted sum in one kernel ---------------------------------------
-// Work-group: 16 rows of every chosen expert's down matrix (16 columns of y). The token's h of all
-// its experts lies in LDS (rows of whole KB, zeros behind each), and every MFMA column holds it: a
-// lane then reads its operand without regard to its column, and column 0 is the result. So only
-// weights pass through the waves' rings, D lines ahead. A wave takes an expert, or one of kc runs
-// of K of it where there are fewer experts than waves; the waves' sums are weighted and added in
-// order, and y is written at once.
-constexpr int kOneWaves = 8, kOneDepth = 6;
-constexpr int kOneH = 48 * 1024;  // most LDS that h may take
+// ---- one token -------------------------------------------------------------------------------
+// The token's operand lies in LDS, and every MFMA column holds it: a lane reads its chunks without
+// regard to its column, and column 0 is the result. So only weights pass through the waves' rings.
+// most LDS that the operand may take (x: two work-groups share a CU)
+constexpr int kOneH = 48 * 1024, kOneX = 8 * 1024;
+constexpr int one_pitch(int64_t n, int bytes) { return (int)((n * bytes + 1023) / 1024 * 1024); }
 
-constexpr int one_pitch(int64_t I, int hbytes) { return (int)((I * hbytes + 1023) / 1024 * 1024); }
+// n bytes of row `pr` of a matrix of rows of rb bytes to LDS, in whole KB with zeros behind: the
+// KBs q, q + W, ... of `rows` such rows, for wave q of W
+template <int W>
+__device__ __forceinline__ void stage_rows(__amdgpu_buffer_rsrc_t r, int rows, int rb, int pitch,
+                                           char* to, int wave, int lane) {
+    const int kbs = pitch >> 10;
+    for (int q = wave; q < rows * kbs; q += W) {
+        const int pr = q / kbs, o = (q - pr * kbs) * 1024 + lane * 16;
+        load_lds16(r, to + q * 1024, o < rb ? pr * rb + o : kOOB, 0);
+    }
+}
+
+// acc[r][p] += the product of RT row tiles and part p of the token over the lines [l0, l1).
+// hbase: LDS address of this lane's chunk of line 0 of part 0, parts `ppitch` apart; staged() is
+// called once the first D lines' loads are issued. The rest as for lines().
+template <typename XT, bool FP8, int RT, int PARTS, int D, typename F>
+__device__ __forceinline__ void lines_one(f32x4_t (&acc)[RT][PARTS], __amdgpu_buffer_rsrc_t wr,
+                                          const int (&woff)[RT][2], int rb, uint32_t hbase,
+                                          int ppitch, const float* const (&sc)[RT], int l0, int l1,
+                                          char* ring, F staged) {
+    using C = Core<XT, FP8>;
+    constexpr int XC = C::XC, L = 2 * RT;
+    static_assert((D - 1) * L <= 63, "outstanding loads");
+    const int lane = threadIdx.x & 63;
+    const int i = lane & 15, g = lane >> 4;
+    const int lcol = ((lane & 7) ^ (lane >> 3)) * 16;
+    auto load = [&](int l, char* at) {
+        const bool in = (l < l1) & (l * kLine + lcol < rb);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                load_lds16<kNonTemporal>(wr, at + (2 * r + h) * 1024,
+                                         (in & (woff[r][h] >= 0)) ? woff[r][h] + lcol : kOOB,
+                                         l * kLine);
+    };
+#pragma unroll
+    for (int t = 0; t < D; ++t) load(l0 + t, ring + t * L * 1024);
+    staged();
+    const uint32_t base = lds_addr(ring) + i * kLine;
+    const uint32_t a0 = base + (g ^ (i & 7)) * 16, a1 = base + ((4 + g) ^ (i & 7)) * 16;
+    int slot = 0;
+    for (int l = l0; l < l1; ++l) {
+        wait_vm_lds<(D - 1) * L>();
+        V16 a[RT][2], b[PARTS][XC][2];
+        lds_tiles<RT, 0>(a0 + slot * L * 1024, a1 + slot * L * 1024, a);
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) {
+            const uint32_t at = hbase + p * ppitch + l * kLine * XC;
+            if constexpr (XC == 1) {
+                lds_tiles<1, 0>(at, at + 64, b[p]);
+            } else {
+                lds_tiles<1, 0>(at, at + 16, b[p]);
+                lds_tiles<1, 128>(at, at + 16, b[p] + 1);
+            }
+        }
+        load(l + D, ring + slot * L * 1024);
+        slot = slot + 1 == D ? 0 : slot + 1;
+        f32x4_t blk[RT][PARTS];
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) blk[r][p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                typename C::vec w[XC];
+                C::widen(a[r][h], w);
+#pragma unroll
+                for (int c = 0; c < XC; ++c)
+#pragma unroll
+                    for (int p = 0; p < PARTS; ++p) {
+                        f32x4_t& t = FP8 ? blk[r][p] : acc[r][p];
+                        t = C::mma(w[c], XC == 1 ? b[p][0][h] : b[p][h * (XC - 1)][c], t);
+                    }
+            }
+        if (FP8) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const float s = sc[r][l];
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[r][p][e] = fmaf(s, blk[r][p][e], acc[r][p][e]);
+            }
+        }
+    }
+    wait_vm_lds<0>();  // the ring is free again
+}
+
+// Gate and up, SiLU(g) * u -> h. Work-group: 16 neurons of the expert of one rank, K split over 4
+// waves. With CHOOSE each work-group makes the token's choice itself, from the logits (the first
+// one also writes ids and weights): the same arithmetic in each, and a launch less.
+constexpr int kOneMaxE = 256;
+
+template <typename XT, bool FP8, bool CHOOSE>
+__global__ __launch_bounds__(256) void moe_gate_up_one(
+    const XT* __restrict__ x, int d, Choice choice, int32_t* __restrict__ ids,
+    float* __restrict__ weights, int k, const uint8_t* __restrict__ gate_up,
+    const float* __restrict__ scales, int E, int I, typename HType<XT, FP8>::type* __restrict__ H,
+    int parts) {
+    constexpr int W = 4, D = 4, RT = 2;
+    __shared__ __align__(1024) char rings[W * D * 2 * RT * 1024];
+    __shared__ ChoiceLds<CHOOSE ? kOneMaxE : 1> cs;
+    extern __shared__ __align__(1024) char hs[];
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
+    const int r = blockIdx.y, n0 = blockIdx.x * 16;
+    constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
+    const int rb = d * WB, xb = d * (int)sizeof(XT);
+    stage_rows<W>(make_rsrc(x, xb), 1, xb, one_pitch(d, sizeof(XT)), hs, wave, lane);
+    int e;
+    if constexpr (CHOOSE) {
+        choose_experts<kOneMaxE>(choice, 0, blockIdx.x == 0 && r == 0, ids, weights, cs);
+        e = __builtin_amdgcn_readfirstlane(cs.id[r]);
+    } else {
+        e = __builtin_amdgcn_readfirstlane(ids[r]);
+    }
+    if ((unsigned)e >= (unsigned)E) {
+        wait_vm_lds<0>();  // no load may land in LDS after the work-group's end
+        return;
+    }
+    const int nl = (rb + kLine - 1) / kLine, nb = (I + 127) / 128;
+    const auto wr = make_rsrc(gate_up + (int64_t)e * 2 * I * rb, (int64_t)2 * I * rb);
+    int woff[RT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int j = n0 + 8 * h + lr;
+        woff[0][h] = j < I ? j * rb : kOOB;
+        woff[1][h] = j < I ? (I + j) * rb : kOOB;
+    }
+    const float* sc[RT];
+    sc[0] = FP8 ? scales + ((int64_t)e * 2 * nb + n0 / 128) * nl : nullptr;
+    sc[1] = FP8 ? sc[0] + (int64_t)nb * nl : nullptr;
+    int l0, l1;
+    wave_lines<W>(nl, wave, l0, l1);
+    f32x4_t acc[RT][1];
+#pragma unroll
+    for (int q = 0; q < RT; ++q) acc[q][0] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    lines_one<XT, FP8, RT, 1, D>(acc, wr, woff, rb, lds_addr(hs) + (FP8 ? 32 * g : 16 * g), 0, sc, l0,
+                                 l1, rings + wave * D * 2 * RT * 1024, [&]() {
+                                     // every wave's part of x has landed (the weights may fly)
+                                     wait_vm_lds<D * 2 * RT>();
+                                     wg_barrier();
+                                 });
+    f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings);
+    __syncthreads();  // the rings are done with
+    if (row == 0) {
+        red[(wave * 2) * 4 + g] = acc[0][0];
+        red[(wave * 2 + 1) * 4 + g] = acc[1][0];
+    }
+    __syncthreads();
+    // thread j: neuron n0 + j
+    const int j = threadIdx.x;
+    if (j < 16 && n0 + j < I) {
+        const float* f = reinterpret_cast<const float*>(red);
+        float sg = f[j], su = f[16 + j];
+#pragma unroll
+        for (int w = 1; w < W; ++w) {
+            sg += f[w * 32 + j];
+            su += f[w * 32 + 16 + j];
+        }
+        put_h(silu_f32(sg) * su, (int64_t)r * I + n0 + j, (int64_t)k * I, parts, H);
+    }
+}
+
+// Down and the weighted sum. Work-group: 16 rows of every chosen expert's down matrix (16 columns
+// of y). A wave takes an expert, or one of kc runs of K of it where there are fewer experts than
+// waves; the waves' sums are weighted and added in order, and y is written at once. (With h in the
+// rings too, as for more tokens, 10.3 us where this takes 7.6: 8 experts of 768 x 2048.)
+constexpr int kOneWaves = 8;
 
 template <typename HT, bool FP8, int PARTS, typename YT>
 __global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
     const HT* __restrict__ H, int d, const int32_t* __restrict__ ids,
     const float* __restrict__ weights, int k, int kc, const uint8_t* __restrict__ down,
     const float* __restrict__ scales, int E, int I, YT* __restrict__ y) {
-    using C = Core<HT, FP8>;
-    constexpr int XC = C::XC, D = kOneDepth, L = 2;
-    __shared__ __align__(1024) char rings[kOneWaves * D * L * 1024];
+    constexpr int D = 6;
+    __shared__ __align__(1024) char rings[kOneWaves * D * 2 * 1024];
     extern __shared__ __align__(1024) char hs[];
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row = lane & 15, g = lane >> 4;
+    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
     const int c0 = blockIdx.x * 16;
     constexpr int WB = FP8 ? 1 : (int)sizeof(HT);
     const int rb = I * WB, hb = I * (int)sizeof(HT), pitch = one_pitch(I, sizeof(HT));
     const int nl = (rb + kLine - 1) / kLine, per = (nl + kc - 1) / kc;
-    char* const ring = rings + wave * D * L * 1024;
-
-    // h to LDS: row r of part p at (p k + r) pitch
-    const auto hr = make_rsrc(H, (int64_t)PARTS * k * I * sizeof(HT));
-    const int kbs = pitch >> 10;
-    for (int q = wave; q < PARTS * k * kbs; q += kOneWaves) {
-        const int pr = q / kbs, o = (q - pr * kbs) * 1024 + lane * 16;
-        load_lds16(hr, hs + q * 1024, o < hb ? pr * hb + o : kOOB, 0);
-    }
-    const int lr = lane >> 3, lcol = ((lane & 7) ^ lr) * 16;
-    const int w0 = c0 + lr < d ? (c0 + lr) * rb + lcol : kOOB;
-    const int w8 = c0 + 8 + lr < d ? (c0 + 8 + lr) * rb + lcol : kOOB;
-    const uint32_t base = lds_addr(ring) + row * kLine;
-    const uint32_t a0 = base + (g ^ (row & 7)) * 16, a1 = base + ((4 + g) ^ (row & 7)) * 16;
-    const uint32_t hbase = lds_addr(hs) + (XC == 1 ? 16 * g : 32 * g);
+    // row r of part p of h at (p k + r) pitch
+    stage_rows<kOneWaves>(make_rsrc(H, (int64_t)PARTS * k * I * sizeof(HT)), PARTS * k, hb, pitch, hs,
+                          wave, lane);
+    const int woff[1][2] = {{c0 + lr < d ? (c0 + lr) * rb : kOOB,
+                             c0 + 8 + lr < d ? (c0 + 8 + lr) * rb : kOOB}};
     bool ready = false;
     f32x4_t tot = {0.0f, 0.0f, 0.0f, 0.0f};
     for (int u = wave; u < k * kc; u += kOneWaves) {
@@ -688,72 +848,28 @@ __global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
         const bool some = (unsigned)e < (unsigned)E;
         const int ex = some ? e : 0;
         const auto wr = make_rsrc(down + (int64_t)ex * d * rb, (int64_t)d * rb);
-        const float* sc = FP8 ? scales + ((int64_t)ex * ((d + 127) / 128) + c0 / 128) * nl : nullptr;
+        const float* sc[1] = {
+            FP8 ? scales + ((int64_t)ex * ((d + 127) / 128) + c0 / 128) * nl : nullptr};
         const int l0 = min(nl, q * per), l1 = some ? min(nl, l0 + per) : l0;
-        auto load = [&](int l, char* at) {
-            const bool in = (l < l1) & (l * kLine + lcol < rb);
-            load_lds16<kNonTemporal>(wr, at, (in & (w0 >= 0)) ? w0 : kOOB, l * kLine);
-            load_lds16<kNonTemporal>(wr, at + 1024, (in & (w8 >= 0)) ? w8 : kOOB, l * kLine);
-        };
+        f32x4_t acc[1][PARTS];
 #pragma unroll
-        for (int t = 0; t < D; ++t) load(l0 + t, ring + t * L * 1024);
-        if (!ready) {
-            // every wave's part of h has landed (the weights' first lines, issued later, may fly)
-            wait_vm_lds<D * L>();
-            wg_barrier();
-            ready = true;
-        }
-        const float f = some ? weights[r] : 0.0f;
-        f32x4_t acc[PARTS];
-#pragma unroll
-        for (int p = 0; p < PARTS; ++p) acc[p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        int slot = 0;
-        for (int l = l0; l < l1; ++l) {
-            wait_vm_lds<(D - 1) * L>();
-            V16 a[1][2], b[PARTS][XC][2];
-            lds_tiles<1, 0>(a0 + slot * L * 1024, a1 + slot * L * 1024, a);
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) {
-                const uint32_t at = hbase + (p * k + r) * pitch + l * kLine * XC;
-                if constexpr (XC == 1) {
-                    lds_tiles<1, 0>(at, at + 64, b[p]);
-                } else {
-                    lds_tiles<1, 0>(at, at + 16, b[p]);
-                    lds_tiles<1, 128>(at, at + 16, b[p] + 1);
-                }
-            }
-            load(l + D, ring + slot * L * 1024);
-            slot = slot + 1 == D ? 0 : slot + 1;
-            f32x4_t blk[PARTS];
-#pragma unroll
-            for (int p = 0; p < PARTS; ++p) blk[p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                typename C::vec w[XC];
-                C::widen(a[0][h], w);
-#pragma unroll
-                for (int c = 0; c < XC; ++c)
-#pragma unroll
-                    for (int p = 0; p < PARTS; ++p) {
-                        f32x4_t& t = FP8 ? blk[p] : acc[p];
-                        t = C::mma(w[c], XC == 1 ? b[p][0][h] : b[p][h * (XC - 1)][c], t);
-                    }
-            }
-            if (FP8) {
-                const float s = sc[l];
-#pragma unroll
-                for (int p = 0; p < PARTS; ++p)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) acc[p][i] = fmaf(s, blk[p][i], acc[p][i]);
-            }
-        }
-        wait_vm_lds<0>();  // the ring is free again
+        for (int p = 0; p < PARTS; ++p) acc[0][p] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+        lines_one<HT, FP8, 1, PARTS, D>(acc, wr, woff, rb,
+                                        lds_addr(hs) + r * pitch + (FP8 ? 32 * g : 16 * g),
+                                        k * pitch, sc, l0, l1, rings + wave * D * 2 * 1024, [&]() {
+                                            if (ready) return;
+                                            // every wave's part of h has landed
+                                            wait_vm_lds<D * 2>();
+                                            wg_barrier();
+                                            ready = true;
+                                        });
         if (some) {
+            const float f = weights[r];
 #pragma unroll
             for (int p = PARTS - 1; p >= 0; --p) {
                 const float fp = std::is_same<HT, f16_t>::value ? f * part_factor<HT>(p) : f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tot[i] = fmaf(fp, acc[p][i], tot[i]);
+                for (int i = 0; i < 4; ++i) tot[i] = fmaf(fp, acc[0][p][i], tot[i]);
             }
         }
     }
@@ -802,8 +918,8 @@ Plan moe_plan(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt, int 
 struct Args {
     const void* x;
     int64_t T, d;
-    const int32_t* ids;
-    const float* w;
+    int32_t* ids;
+    float* w;
     int64_t k;
     const uint8_t* gate_up;
     const float* gus;
@@ -814,6 +930,7 @@ struct Args {
     int ydt;
     void* ws;
     Plan p;
+    const Choice* choice;
     hipStream_t s;
 };
 
@@ -841,17 +958,29 @@ void experts(const Args& a) {
     const int gl = (int)((a.d * (FP8 ? 1 : (int)sizeof(XT)) + kLine - 1) / kLine);
     const int dl = (int)((a.I * (FP8 ? 1 : (int)sizeof(HT)) + kLine - 1) / kLine);
     const XT* x = static_cast<const XT*>(a.x);
-    // Long rows: more waves along K, so that fewer work-groups take more of a row at a time
-    if (gl >= kLongRow)
+    const int64_t xlds = one_pitch(a.d, sizeof(XT));
+    if (a.T == 1 && xlds <= kOneX) {
+        const dim3 grid((unsigned)((a.I + 15) / 16), (unsigned)a.k);
+        if (a.choice)
+            moe_gate_up_one<XT, FP8, true><<<grid, 256, (size_t)xlds, a.s>>>(
+                x, (int)a.d, *a.choice, a.ids, a.w, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I,
+                H, a.p.parts);
+        else
+            moe_gate_up_one<XT, FP8, false><<<grid, 256, (size_t)xlds, a.s>>>(
+                x, (int)a.d, Choice{}, a.ids, a.w, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, H,
+                a.p.parts);
+    } else if (gl >= kLongRow) {
+        // long rows: more waves along K, so that fewer work-groups take more of a row at a time
         moe_gate_up<XT, FP8, 16 * 1024, 4, 1, 1>
             <<<dim3((unsigned)((a.I + 15) / 16), slots), 256, lds, a.s>>>(
                 x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
                 H, a.p.parts);
-    else
+    } else {
         moe_gate_up<XT, FP8, 24 * 1024, 2, 1, 1>
             <<<dim3((unsigned)((a.I + 15) / 16), slots), 128, lds, a.s>>>(
                 x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
                 H, a.p.parts);
+    }
     const int64_t hlds = (int64_t)PARTS * a.k * one_pitch(a.I, sizeof(HT));
     if (a.T == 1 && hlds <= kOneH) {
         // one token: as many runs of K as keep the waves busy
@@ -896,13 +1025,17 @@ bool moe_supported(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt,
     return 2 * I * d * wb <= top && T * d * 4 <= top && p.pairs * I * p.parts * p.hbytes <= top;
 }
 
-hipError_t launch_moe(const void* x, int xdt, int64_t T, int64_t d, const int32_t* ids,
-                      const float* w, int64_t k, const void* gate_up, const float* gus,
-                      const void* down, const float* dns, int64_t E, int64_t I, int wdt, void* y,
-                      int ydt, void* ws, hipStream_t s) {
+bool moe_chooses(int64_t T, int64_t d, int64_t E, int xdt) {
+    return T == 1 && E <= kOneMaxE && one_pitch(d, xdt == 0 ? 4 : 2) <= kOneX;
+}
+
+hipError_t launch_moe(const void* x, int xdt, int64_t T, int64_t d, int32_t* ids, float* w,
+                      int64_t k, const void* gate_up, const float* gus, const void* down,
+                      const float* dns, int64_t E, int64_t I, int wdt, void* y, int ydt, void* ws,
+                      hipStream_t s, const Choice* choice) {
     const Args a{x, T, d, ids, w, k, static_cast<const uint8_t*>(gate_up), gus,
                  static_cast<const uint8_t*>(down), dns, E, I, y, ydt, ws,
-                 moe_plan(T, k, d, I, xdt, wdt, ydt), s};
+                 moe_plan(T, k, d, I, xdt, wdt, ydt), choice, s};
     const bool three = a.p.parts == 3;
     if (wdt == 0)
         experts<float, false, 1>(a);

@@ -13,6 +13,7 @@
 #include "common.h"
 #include "launch.h"
 #include "mfma.h"
+#include "route.h"
 
 namespace si {
 
@@ -113,105 +114,11 @@ __global__ __launch_bounds__(kLogitWaves * 64) void route_logits(
 
 // ---- choice ------------------------------------------------------------------------------
 
-// order key: unsigned order equals the order of the values, -0 = +0, NaN below every number
-__device__ __forceinline__ uint64_t key_of(double v) {
-    if (!(v == v)) return 1u;
-    v += 0.0;  // -0 -> +0
-    const uint64_t u = (uint64_t)__double_as_longlong(v);
-    return (u >> 63) ? ~u : (u | 0x8000000000000000ull);
-}
-
-// Fixed-order sum or maximum over the work-group's values
-template <bool MAX>
-__device__ __forceinline__ double group_reduce(double v, double* red) {
-#pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) {
-        const double o = __shfl_xor(v, m, kWave);
-        v = MAX ? fmax(v, o) : v + o;
-    }
-    const int n = blockDim.x >> 6;
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = red[0];
-    for (int i = 1; i < n; ++i) v = MAX ? fmax(v, red[i]) : v + red[i];
-    return v;
-}
-
-// One work-group a token. Thread i < EP owns expert i (EP: E rounded up to a power of two); an
-// expert's rank is the number of experts before it in the order, counted by blockDim / EP threads
-// an expert from the keys in LDS: one exchange, where k rounds of a maximum over the work-group
-// would take several each. Softmax weights that are divided by their chosen sum need no sum over
-// the others: exp(z - top) / sum of the chosen, with the scores of k experts only.
-__global__ __launch_bounds__(1024) void route_choose(
-    const double* __restrict__ part, int KS, int T, int E, int EP, const float* __restrict__ bias,
-    int k, int sigmoid, int renorm, float scale, const int32_t* __restrict__ n_valid,
-    int32_t* __restrict__ ids, float* __restrict__ weights) {
-    __shared__ uint64_t keys[1024];
-    __shared__ int rank[1024];
-    __shared__ double red[16];
-    __shared__ double chosen[32];
-    const int t = blockIdx.x, i = threadIdx.x;
-    if (n_valid && t >= *n_valid) {
-        if (i < k) {
-            ids[(int64_t)t * k + i] = -1;
-            weights[(int64_t)t * k + i] = 0.0f;
-        }
-        return;
-    }
-    const bool mine = i < E;
-    double z = 0.0;
-    if (mine)
-        for (int s = 0; s < KS; ++s) z += part[((int64_t)s * T + t) * E + i];
-    // the score of a softmax by its logit alone, until the chosen are known
-    const bool late = !sigmoid && renorm && !bias;
-    double p = z;
-    if (sigmoid) {
-        p = 1.0 / (1.0 + exp(-z));
-    } else if (!late) {
-        const double top = group_reduce<true>(mine ? z : -HUGE_VAL, red);
-        p = mine ? exp(z - top) : 0.0;
-        p /= group_reduce<false>(p, red);
-    }
-    if (i < EP) {
-        keys[i] = mine ? key_of(bias ? p + (double)bias[i] : z) : 0u;  // 0: below every expert's
-        rank[i] = 0;
-    }
-    const bool nan = __syncthreads_or(mine && !(z == z));
-    // thread i counts for expert i % EP over the i / EP-th part of the experts
-    const int me = i & (EP - 1);
-    if (me < E) {
-        const int parts = (int)blockDim.x / EP, per = (E + parts - 1) / parts;
-        const int lo = min(E, (i / EP) * per), hi = min(E, lo + per);
-        const uint64_t m = keys[me];
-        int n = 0;
-#pragma unroll 8
-        for (int j = lo; j < hi; ++j) n += keys[j] > m - (uint64_t)(j < me);
-        if (n) atomicAdd(&rank[me], n);  // whole numbers: the order of the additions is free
-    }
-    __syncthreads();
-    const int r = mine ? rank[i] : k;
-    if (r < k) {
-        chosen[r] = p;
-        ids[(int64_t)t * k + r] = i;
-    }
-    __syncthreads();
-    if (late) {
-        // (a NaN logit makes every score NaN, as in the softmax over all experts)
-        const double top = chosen[0];
-        const double e = i < k ? (nan ? __longlong_as_double(0x7ff8000000000000ll)
-                                      : exp(chosen[i] - top))
-                               : 0.0;
-        __syncthreads();
-        if (i < k) chosen[i] = e;
-        __syncthreads();
-    }
-    if (i >= k) return;  // thread i: the expert of rank i
-    double w = chosen[i], sum = 0.0;
-    if (renorm)
-        for (int j = 0; j < k; ++j) sum += chosen[j];
-    if (renorm) w = sum > 0.0 || !(sum == sum) ? w / sum : 0.0;
-    weights[(int64_t)t * k + i] = (float)(w * (double)scale);
+// One work-group a token
+__global__ __launch_bounds__(1024) void route_choose(Choice a, int32_t* __restrict__ ids,
+                                                    float* __restrict__ weights) {
+    __shared__ ChoiceLds<1024> s;
+    choose_experts<1024>(a, blockIdx.x, true, ids, weights, s);
 }
 
 template <typename XT, typename WT>
@@ -241,10 +148,9 @@ size_t route_workspace(int64_t T, int64_t E, int64_t d) {
     return (size_t)route_chunks(T, E, d) * T * E * sizeof(double);
 }
 
-hipError_t launch_route(const void* x, int xdt, int64_t T, int64_t d, const void* w, int wdt,
-                        int64_t E, const float* bias, int64_t k, int sigmoid, int renorm,
-                        float scale, const int32_t* n_valid, int32_t* ids, float* weights,
-                        void* ws, hipStream_t s) {
+Choice route_logits_of(const void* x, int xdt, int64_t T, int64_t d, const void* w, int wdt,
+                       int64_t E, const float* bias, int64_t k, int sigmoid, int renorm,
+                       float scale, const int32_t* n_valid, void* ws, hipStream_t s) {
     const int KS = route_chunks(T, E, d);
     // chunks of whole 64-value runs of the waves (whole lines of 16-bit data)
     constexpr int kRun = 64 * kLogitWaves;
@@ -262,9 +168,12 @@ hipError_t launch_route(const void* x, int xdt, int64_t T, int64_t d, const void
         logits<f16_t, float>(x, w, T, E, d, kchunk, KS, part, s);
     int EP = 64;
     while (EP < E) EP *= 2;
-    const int threads = EP <= 128 ? 512 : 1024;
-    route_choose<<<dim3((unsigned)T), threads, 0, s>>>(part, KS, (int)T, (int)E, EP, bias, (int)k,
-                                                   sigmoid, renorm, scale, n_valid, ids, weights);
+    return Choice{part, KS, (int)T, (int)E, EP, bias, (int)k, sigmoid, renorm, scale, n_valid};
+}
+
+hipError_t launch_choose(const Choice& c, int32_t* ids, float* weights, hipStream_t s) {
+    // more threads an expert where there are many to compare
+    route_choose<<<dim3((unsigned)c.T), c.EP <= 128 ? 512 : 1024, 0, s>>>(c, ids, weights);
     return hipGetLastError();
 }
 

@@ -6,6 +6,8 @@
 
 namespace si {
 
+struct Choice;  // route.h
+
 // ---- k_decode.hip: per-token path ------------------------------------------------------
 // Input of a stacked layer given as the previous layer's pair: x = RMSNorm(x_prev + y_prev),
 // unit gain, computed in the prologue of the per-token kernel and stored to x_out (float32 or
@@ -163,15 +165,20 @@ hipError_t launch_matmul_fp8(const uint8_t* x, const float* xs, int64_t M, int64
 
 // ---- k_route.hip, k_moe.hip: mixture of experts -------------------------------------------
 size_t route_workspace(int64_t T, int64_t E, int64_t d);
-hipError_t launch_route(const void* x, int xdt, int64_t T, int64_t d, const void* w, int wdt,
-                        int64_t E, const float* bias, int64_t k, int sigmoid, int renorm,
-                        float scale, const int32_t* n_valid, int32_t* ids, float* weights,
-                        void* ws, hipStream_t s);
+// enqueues the logits (float64 partial sums in ws); what the choice of the experts then takes
+Choice route_logits_of(const void* x, int xdt, int64_t T, int64_t d, const void* w, int wdt,
+                       int64_t E, const float* bias, int64_t k, int sigmoid, int renorm,
+                       float scale, const int32_t* n_valid, void* ws, hipStream_t s);
+hipError_t launch_choose(const Choice& c, int32_t* ids, float* weights, hipStream_t s);
 size_t moe_workspace(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt, int ydt);
 bool moe_supported(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt, int ydt);
-hipError_t launch_moe(const void* x, int xdt, int64_t T, int64_t d, const int32_t* ids,
-                      const float* w, int64_t k, const void* gate_up, const float* gus,
-                      const void* down, const float* dns, int64_t E, int64_t I, int wdt, void* y,
-                      int ydt, void* ws, hipStream_t s);
+// whether launch_moe makes the choice of the experts itself (in its first kernel)
+bool moe_chooses(int64_t T, int64_t d, int64_t E, int xdt);
+// choice (with moe_chooses): the experts are chosen from it, and ids and w are written; else they
+// are read
+hipError_t launch_moe(const void* x, int xdt, int64_t T, int64_t d, int32_t* ids, float* w,
+                      int64_t k, const void* gate_up, const float* gus, const void* down,
+                      const float* dns, int64_t E, int64_t I, int wdt, void* y, int ydt, void* ws,
+                      hipStream_t s, const Choice* choice = nullptr);
 
 }  // namespace si

@@ -152,6 +152,10 @@ LAYERS = [
     (1, 8, 2, 64, 48), (1, 4, 4, 272, 16), (2, 16, 3, 128, 400), (5, 6, 6, 144, 144),
     (13, 64, 6, 256, 208), (16, 2, 1, 528, 336), (17, 1, 1, 64, 32), (40, 3, 2, 160, 272),
     (70, 2, 2, 96, 64), (130, 5, 1, 64, 128),
+    # one token: a choice of its own launch, h past the LDS kept for it, x past it, many ranks
+    (1, 300, 3, 64, 48), (1, 200, 6, 64, 2064), (1, 16, 10, 4368, 32), (1, 256, 32, 256, 16),
+    # long rows
+    (3, 4, 2, 8208, 16), (3, 4, 2, 48, 8208),
 ]
 
 
