@@ -187,8 +187,10 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
     constexpr int LA = BN / 8 / NW, LB = BM / 8 / NW;  // 8-row loads of a wave
     static_assert(LA * NW * 8 == BN && LB * NW * 8 == BM && TN <= kBlk && kBlk % TN == 0, "tile");
     static_assert(S >= 2 && S <= 4 && BM % 64 == 0 && RN % 2 == 0, "stages");
-    constexpr int kScale = (BN + BM) * kBlk;      // the tokens' scales behind the rows
-    constexpr int kStage = kScale + BM * 4;
+    constexpr int kScale = (BN + BM) * kBlk;      // the tokens' scales behind the rows, and the
+    constexpr int kWScale = kScale + BM * 4;      // weight rows' behind them
+    constexpr int kStage = kWScale + 256;
+    static_assert(NW > BM / 64, "a wave for the weights' scales");
     // one array a stage: the compiler must see that a step's reads and loads do not alias, or it
     // waits for the loads it has just issued
     __shared__ __align__(1024) char s0[kStage];
@@ -237,10 +239,13 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
     }
 #pragma unroll
     for (int t = 0; t < LB; ++t) vb[t] = ((wave * LB + t) * 8 + lrow) * K + lcol;
-    // every wave loads 64 tokens' scales (more than one wave the same ones where BM < 64 NW), so
-    // that all count the same loads
-    const int sg = wave % (BM / 64);
-    const int vs = (64 * sg + lane) * kb * 4;
+    // Waves below BM / 64 load 64 tokens' scales each, the others the scales of the tile's row
+    // blocks (all the same ones), so that all count the same loads. (As scalar loads these would
+    // hold up every wait for LDS reads of their step: they are counted together, out of order.)
+    const int sg = wave < BM / 64 ? wave : BM / 64;
+    constexpr int kRowBlocks = BN > kBlk ? BN / kBlk : 1;
+    const int vs = wave < BM / 64 ? (64 * wave + lane) * kb * 4
+                                  : (lane < kRowBlocks ? lane * kb * 4 : kOOB);
 
     // The tiles that an XCD works on at a time read the same rows in step, so that each step's
     // lines would be first read, by all of them, one step before their use. Each of them also
@@ -259,7 +264,9 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
         const int nr = c.id < 0 ? 0 : min(BN, N - n0), mr = c.id < 0 ? 0 : min(BM, M - m0);
         lw = make_rsrc(w + (int64_t)n0 * K, (int64_t)nr * K);
         lx = make_rsrc(x + (int64_t)m0 * K, (int64_t)mr * K);
-        ls = make_rsrc(xs + (int64_t)m0 * kb, (int64_t)mr * kb * 4);
+        const int nbl = nr == 0 ? 0 : min(kRowBlocks, (N - 1) / kBlk - n0 / kBlk + 1);
+        ls = make_rsrc(wave < BM / 64 ? xs + (int64_t)m0 * kb : ws + (int64_t)(n0 / kBlk) * kb,
+                       (int64_t)(wave < BM / 64 ? mr : nbl) * kb * 4);
         const int q = (int)threadIdx.x;
         const int rr = min((c.tn % sharex) * rx + q, max(mr - 1, 0));
         const int rs = min((c.tm % sharew) * rw + max(min(q - rx, rw - 1), 0), max(nr - 1, 0));
@@ -288,7 +295,7 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
     // operand reads: row i of a tile, chunks g and 4 + g
     const int o0 = i * kBlk + (g ^ (i & 7)) * 16, o1 = o0 ^ 64;
     const int oa = wn * TN * kBlk, ob = BN * kBlk + wm * TM * kBlk;
-    const int os = kScale + (wm * TM + i) * 4;
+    const int os = kScale + (wm * TM + i) * 4, ow = kWScale + wn * TN / kBlk * 4;
 
     // A step meets its barrier before the products of its last row tile: by then every wave has
     // read the whole stage, so the loads of S steps on may overwrite it, and the next step's
@@ -296,7 +303,7 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
     typename Op<EXACT>::type vx[RM];
     V16 xlo[RM], xhi[RM], lo[2], hi[2];
     f32x4_t t[2][RM];
-    float sc[RM], sp[RM], sraw[RM], sw, swn;
+    float sc[RM], sp[RM], sraw[RM], sw;
     auto row_tile = [&](const char* at, int n) {
         lo[n & 1] = ld16(at + oa + n * 16 * kBlk + o0);
         hi[n & 1] = ld16(at + oa + n * 16 * kBlk + o1);
@@ -305,12 +312,12 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
         xlo[m] = ld16(at + ob + m * 16 * kBlk + o0);
         xhi[m] = ld16(at + ob + m * 16 * kBlk + o1);
         sraw[m] = *reinterpret_cast<const float*>(at + os + 64 * m);
+        if (m == 0) sw = *reinterpret_cast<const float*>(at + ow);
     };
     auto add = [&](int n, int m, const float* f) {
 #pragma unroll
         for (int e = 0; e < 4; ++e) acc[n][m][e] = fmaf(f[m], t[n & 1][m][e], acc[n][m][e]);
     };
-    int wnext;  // index of the weights' scale of the step after this one
     auto step = [&](char* cur, const char* nxt) {
 #pragma unroll
         for (int m = 0; m < RM; ++m) {
@@ -318,7 +325,6 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
             sp[m] = sc[m];
             sc[m] = sraw[m] * sw;
         }
-        swn = ws[wnext];
 #pragma unroll
         for (int n = 0; n < RN; ++n) {
             const bool last = n + 1 == RN;
@@ -352,10 +358,6 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-        sw = swn;
-    };
-    auto wscale = [&](const Item& c) {
-        return __builtin_amdgcn_readfirstlane((min(c.tn * BN + wn * TN, N - 1) / kBlk) * kb + c.b0);
     };
     Item it = item_at((int)blockIdx.x);
     if (it.id < 0) return;
@@ -364,8 +366,6 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
     load(s1);
     if (S > 2) load(s2);
     if (S > 3) load(s3);
-    wnext = wscale(it);
-    sw = ws[wnext];
     wait_vm_lds<(S - 1) * kLoads + (TOUCH ? 1 : 0)>();
     wg_barrier();
     row_tile(s0, 0);
@@ -380,19 +380,13 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
             for (int n = 0; n < RN; ++n) acc[n][m] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
         }
         const Item next = item_at(it.id + (int)gridDim.x);
-        const int wthen = wscale(next), wlast = wnext + (it.b1 - it.b0 - 1);
         int steps = rounds(it) * S;
-        auto one = [&](char* cur, const char* nxt) {
-            --steps;
-            wnext = steps == 0 ? wthen : (wnext < wlast ? wnext + 1 : wnext);
-            step(cur, nxt);
-        };
-        while (steps > 0) {
+        for (; steps > 0; steps -= S) {
             if (steps == S) aim(next);  // the last round's loads are the next item's first
-            one(s0, s1);
-            one(s1, S == 2 ? s0 : s2);
-            if (S > 2) one(s2, S == 3 ? s0 : s3);
-            if (S > 3) one(s3, s0);
+            step(s0, s1);
+            step(s1, S == 2 ? s0 : s2);
+            if (S > 2) step(s2, S == 3 ? s0 : s3);
+            if (S > 3) step(s3, s0);
         }
 #pragma unroll
         for (int m = 0; m < RM; ++m) add(RN - 1, m, sc);
@@ -496,7 +490,7 @@ void tiles(const Fp8Plan& p, const uint8_t* x, const float* xs, int64_t M, int64
     constexpr int BN = kTiles[T].bn, BM = kTiles[T].bm;
     const int ntm = (int)((M + BM - 1) / BM), ntn = (int)((N + BN - 1) / BN);
     const int64_t items = ((int64_t)ntm * ntn + 7) / 8 * 8 * p.ks;
-    constexpr int kFit = S * ((BN + BM) * kBlk + BM * 4) > 80000 ? 1 : 2;  // by LDS
+    constexpr int kFit = S * ((BN + BM) * kBlk + BM * 4 + 256) > 80000 ? 1 : 2;  // by LDS
     const int64_t most = (int64_t)current_cu_count() * kFit;
     const unsigned grid = (unsigned)(items < most ? items : most);
     if (p.ks == 1) {
