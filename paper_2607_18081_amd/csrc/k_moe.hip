@@ -359,7 +359,7 @@ __device__ __forceinline__ void join_waves(const f32x4_t* acc, f32x4_t* red, int
 }
 
 // ---- gate and up, SiLU(g) * u -> h ---------------------------------------------------------
-// Work-group: WR groups of 16 neurons (their gate and up rows) of one expert, K split over WK waves.
+// Work-group: 16 NR neurons (their gate and up rows) of one expert, K split over WK waves.
 template <typename XT, bool FP8, int RING, int WK, int NR, int NT>
 __device__ __forceinline__ void gate_up_pass(
     const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
@@ -445,28 +445,26 @@ __device__ __forceinline__ void gate_up_pass(
     }
 }
 
-template <typename XT, bool FP8, int RING, int WK, int WR, int NR>
-__global__ __launch_bounds__(WK * WR * 64) void moe_gate_up(
+template <typename XT, bool FP8, int RING, int WK, int NR>
+__global__ __launch_bounds__(WK * 64) void moe_gate_up(
     const XT* __restrict__ x, int64_t T, int d, const int32_t* __restrict__ ids, int npairs, int k,
     const uint8_t* __restrict__ gate_up, const float* __restrict__ scales, int E, int I,
     int by_pair, typename HType<XT, FP8>::type* __restrict__ H, int parts) {
     extern __shared__ uint16_t list[];
-    constexpr int W = WK * WR;
     constexpr int MT = max_tiles<RING, FP8, 2 * NR, 1>();
-    __shared__ __align__(1024) char rings[W * RING];
-    __shared__ int cnt[W];
+    __shared__ __align__(1024) char rings[WK * RING];
+    __shared__ int cnt[WK];
     int e;
-    const int m = expert_pairs<W>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
+    const int m = expert_pairs<WK>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
     if (m == 0) return;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int wr = wave / WK, wk = wave - wr * WK;
+    const int wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
     const uint8_t* gu = gate_up + (int64_t)e * 2 * I * d * WB;
     const float* gs = FP8 ? scales + (int64_t)e * 2 * ((I + 127) / 128) * ((d + 127) / 128) : nullptr;
-    const int n0 = (blockIdx.x * WR + wr) * 16 * NR;
+    const int n0 = blockIdx.x * 16 * NR;
     const int64_t plane = (int64_t)npairs * I;
-    char* const ring = rings + wave * RING;
-    f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings + wr * WK * RING);
+    char* const ring = rings + wk * RING;
+    f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings);
     const int64_t xb = T * d * (int64_t)sizeof(XT);
     for (int c = 0; c < m; c += 16 * MT) {
         const int mc = min(m - c, 16 * MT);
@@ -941,8 +939,18 @@ void sum(const Args& a, YT* y) {
         z, a.ids, a.w, (int)a.k, (int)a.E, (int)a.d, y);
 }
 
-// lines of a weight row from which it counts as long
+// Lines of a weight row from which it counts as long: more waves then share one row group, so that
+// fewer work-groups take more of a row at a time (48 tokens over 8 experts of 14336 x 4096: gate and
+// up by 4 waves 525 us a layer, by 2 542; down by 2 518, by 1 541; 13 tokens over 8-bit experts with
+// rows of 1408, 11 lines: down by 1 wave 159, by 2 187).
 constexpr int kLongRow = 64;
+
+// Pairs an expert from which the tokens' operand, which every wave loads for its own rows, weighs
+// more than the weights: tiles of twice the rows for 64 tokens (8 experts of 4096 x 4096, bf16, 24
+// pairs an expert 197 us by the small tiles and 203 by the large, 64 pairs 445 and 312; 8-bit
+// experts 163 and 145, 342 and 265; 16 pairs an expert, 128 experts of 768 x 2048: 327 and 355).
+// float32 products are bound by their MFMAs, where the large tiles are no help (398 and 723 us).
+constexpr int64_t kManyPairs = 28;
 
 template <typename XT, bool FP8, int PARTS>
 void experts(const Args& a) {
@@ -957,6 +965,7 @@ void experts(const Args& a) {
     const size_t lds = ((size_t)np * sizeof(uint16_t) + 15) / 16 * 16;
     const int gl = (int)((a.d * (FP8 ? 1 : (int)sizeof(XT)) + kLine - 1) / kLine);
     const int dl = (int)((a.I * (FP8 ? 1 : (int)sizeof(HT)) + kLine - 1) / kLine);
+    const bool many = sizeof(XT) == 2 && (int64_t)np >= kManyPairs * a.E;
     const XT* x = static_cast<const XT*>(a.x);
     const int64_t xlds = one_pitch(a.d, sizeof(XT));
     if (a.T == 1 && xlds <= kOneX) {
@@ -969,17 +978,18 @@ void experts(const Args& a) {
             moe_gate_up_one<XT, FP8, false><<<grid, 256, (size_t)xlds, a.s>>>(
                 x, (int)a.d, Choice{}, a.ids, a.w, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, H,
                 a.p.parts);
-    } else if (gl >= kLongRow) {
-        // long rows: more waves along K, so that fewer work-groups take more of a row at a time
-        moe_gate_up<XT, FP8, 16 * 1024, 4, 1, 1>
-            <<<dim3((unsigned)((a.I + 15) / 16), slots), 256, lds, a.s>>>(
-                x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
-                H, a.p.parts);
     } else {
-        moe_gate_up<XT, FP8, 24 * 1024, 2, 1, 1>
-            <<<dim3((unsigned)((a.I + 15) / 16), slots), 128, lds, a.s>>>(
+        auto gate = [&](auto kernel, int rows, int threads) {
+            kernel<<<dim3((unsigned)((a.I + rows - 1) / rows), slots), threads, lds, a.s>>>(
                 x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
                 H, a.p.parts);
+        };
+        if (many)
+            gate(moe_gate_up<XT, FP8, 48 * 1024, 2, 2>, 32, 128);
+        else if (gl >= kLongRow)
+            gate(moe_gate_up<XT, FP8, 16 * 1024, 4, 1>, 16, 256);
+        else
+            gate(moe_gate_up<XT, FP8, 24 * 1024, 2, 1>, 16, 128);
     }
     const int64_t hlds = (int64_t)PARTS * a.k * one_pitch(a.I, sizeof(HT));
     if (a.T == 1 && hlds <= kOneH) {
@@ -997,14 +1007,16 @@ void experts(const Args& a) {
             one(static_cast<XT*>(a.y));
         return;
     }
-    if (dl >= kLongRow)
-        moe_down<HT, FP8, PARTS, 24 * 1024, 2, 2, 2>
-            <<<dim3((unsigned)((a.d + 63) / 64), slots), 256, lds, a.s>>>(
-                H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
+    auto down = [&](auto kernel, int rows, int threads) {
+        kernel<<<dim3((unsigned)((a.d + rows - 1) / rows), slots), threads, lds, a.s>>>(
+            H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
+    };
+    if (many)
+        down(moe_down<HT, FP8, PARTS, 48 * 1024, 1, 2, 4>, 128, 128);
+    else if (dl >= kLongRow)
+        down(moe_down<HT, FP8, PARTS, 24 * 1024, 2, 2, 2>, 64, 256);
     else
-        moe_down<HT, FP8, PARTS, 24 * 1024, 1, 2, 2>
-            <<<dim3((unsigned)((a.d + 63) / 64), slots), 128, lds, a.s>>>(
-                H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
+        down(moe_down<HT, FP8, PARTS, 24 * 1024, 1, 2, 2>, 64, 128);
     if (a.ydt == 0)
         sum(a, static_cast<float*>(a.y));
     else if constexpr (sizeof(XT) == 2)

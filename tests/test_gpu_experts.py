@@ -66,6 +66,27 @@ def test_route(T, E, k, d, xdt, wdt, score):
     _check_route(x, w, k, ids2, weights2, bias=b, score=score, renorm=False, scale=2.5)
 
 
+@pytest.mark.parametrize("T,E,k", [(1, 24, 3), (9, 300, 5)])
+@pytest.mark.parametrize("score,biased", [("softmax", True), ("sigmoid", False)])
+def test_route_modes(T, E, k, score, biased):
+    """A choice bias on softmax scores, sigmoid scores without one; weights with and without their
+    sum, and scaled; the same from the whole layer, which makes the choice elsewhere."""
+    say(f"route modes T={T} E={E} {score} bias={biased}")
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(T, 64, generator=g).to(torch.bfloat16).to(DEV)
+    w = (torch.randn(E, 64, generator=g) / 8).to(DEV)
+    bias = (0.3 * torch.randn(E, generator=g)).to(DEV) if biased else None
+    gu = torch.zeros(E, 2, 16, 64, dtype=torch.bfloat16, device=DEV)
+    dn = torch.zeros(E, 64, 16, dtype=torch.bfloat16, device=DEV)
+    for renorm, scale in ((True, 1.0), (True, -2.0), (False, 0.5)):
+        kw = dict(bias=bias, score=score, renorm=renorm, scale=scale)
+        ids, weights = si.moe_route(x, w, k, **kw)
+        ref = dict(kw, bias=None if bias is None else bias.cpu().numpy())
+        _check_route(x, w, k, ids, weights, **ref)
+        _, ids2, weights2 = si.moe_layer(x, w, gu, dn, k, **kw)
+        assert torch.equal(ids2, ids) and torch.equal(weights2, weights)
+
+
 @pytest.mark.parametrize("xdt", ["bf16", "f16", "f32"])
 @pytest.mark.parametrize("T,E,k,d", [(1, 16, 4, 64), (5, 200, 20, 320), (40, 1000, 32, 1040)])
 def test_route_ties(T, E, k, d, xdt):
@@ -154,8 +175,8 @@ LAYERS = [
     (70, 2, 2, 96, 64), (130, 5, 1, 64, 128),
     # one token: a choice of its own launch, h past the LDS kept for it, x past it, many ranks
     (1, 300, 3, 64, 48), (1, 200, 6, 64, 2064), (1, 16, 10, 4368, 32), (1, 256, 32, 256, 16),
-    # long rows
-    (3, 4, 2, 8208, 16), (3, 4, 2, 48, 8208),
+    # long rows; the most tokens and pairs
+    (3, 4, 2, 8208, 16), (3, 4, 2, 48, 8208), (512, 20, 16, 64, 32),
 ]
 
 
@@ -232,6 +253,22 @@ def test_values_stay_in_their_token():
     assert torch.equal(y[~touched], clean[~touched])
     assert torch.all(torch.isnan(y[3])) and torch.all(torch.isnan(y[ids[:, 0] == 2]))
     assert not torch.any(torch.isfinite(y[8]))
+
+
+@pytest.mark.parametrize("T", [1, 5])
+def test_nan_codes(T):
+    """A NaN code, or a NaN scale, of an 8-bit expert reaches the tokens that use it and no other."""
+    say(f"layer: NaN codes T={T}")
+    E, d, inter = 3, 64, 48
+    dev, _, _ = _experts(E, d, inter, "bf16", "fp8", 9)
+    x = torch.randn(T, d, generator=torch.Generator().manual_seed(T)).to(torch.bfloat16).to(DEV)
+    run = lambda e: si.moe_ffn(x, torch.full((T, 1), e, dtype=torch.int32, device=DEV),  # noqa: E731
+                               torch.ones(T, 1, device=DEV), dev[0], dev[1], dev[2], dev[3])
+    clean = run(0)
+    dev[0].view(torch.uint8)[1, 0, 3, 5] = 0x7f
+    dev[3][2, 0, 0] = float("nan")
+    assert torch.equal(run(0), clean)
+    assert torch.all(torch.isnan(run(1))) and torch.all(torch.isnan(run(2)))
 
 
 @pytest.mark.parametrize("dt", ["f16", "bf16"])
