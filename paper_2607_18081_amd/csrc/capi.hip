@@ -183,14 +183,21 @@ bool valid_route_mode(int mode) {
     return score == SI_ROUTE_SOFTMAX || score == SI_ROUTE_SIGMOID;
 }
 
+// sizes within which the plans below stay in their types
+bool route_sizes(int64_t T, int64_t E, int64_t d) {
+    return T <= 65535 && E <= 1024 && d <= kMaxDim;
+}
+bool fp8_sizes(int64_t M, int64_t N, int64_t K) {
+    return K <= (1 << 20) && M <= (1 << 24) && N <= (1 << 24) && M * N <= ((int64_t)1 << 40);
+}
+
 // sizes and types of si_moe_route; T may be 0
 int check_route(si_dtype xdt, int64_t T, int64_t d, si_dtype rdt, int64_t E, int64_t k, int mode,
                 float scale) {
     if (T < 0 || d < 1 || E < 1 || k < 1 || k > E) return SI_ERR_INVALID;
     if (!valid_route_mode(mode) || !(scale - scale == 0.0f)) return SI_ERR_INVALID;
     if (!valid_dtype(xdt) || (rdt != xdt && rdt != SI_F32)) return SI_ERR_UNSUPPORTED;
-    if (T > 65535 || E > 1024 || k > kMaxPicks || d > kMaxDim || !whole_rows(d, xdt))
-        return SI_ERR_UNSUPPORTED;
+    if (!route_sizes(T, E, d) || k > kMaxPicks || !whole_rows(d, xdt)) return SI_ERR_UNSUPPORTED;
     return SI_OK;
 }
 
@@ -201,8 +208,9 @@ int check_experts(si_dtype xdt, int64_t T, int64_t d, int64_t k, int64_t E, int6
     if (!valid_dtype(xdt) || !(wdt == xdt || (wdt == SI_E4M3 && xdt != SI_F32)))
         return SI_ERR_UNSUPPORTED;
     if (ydt != SI_F32 && ydt != xdt) return SI_ERR_UNSUPPORTED;
-    if (T > kMaxTokens || k > kMaxPicks || T * k > kMaxPairs || E > 65535 || d > kMaxDim || I > kMaxDim ||
-        !whole_rows(d, wdt) || !whole_rows(I, wdt) || !si::moe_supported(T, k, d, I, xdt, wdt, ydt))
+    if (T > kMaxTokens || k > kMaxPicks || T * k > kMaxPairs || E > 65535 || d > kMaxDim ||
+        I > kMaxDim || !whole_rows(d, wdt) || !whole_rows(I, wdt) ||
+        !si::moe_supported(T, k, d, I, xdt, wdt, ydt))
         return SI_ERR_UNSUPPORTED;
     return SI_OK;
 }
@@ -485,10 +493,10 @@ int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C
     if (!valid_dtype(xdt)) return SI_ERR_UNSUPPORTED;
     if (C % 16 != 0) return SI_ERR_UNSUPPORTED;
     if (G == 0 || R == 0) return SI_OK;
-    // no product below leaves 64 bits
+    // no product below leaves 64 bits, and a launch holds fewer than 2^32 threads
     constexpr int64_t top = (int64_t)1 << 31;
-    if (G > top || R > top || C > top || G > ((int64_t)1 << 40) / R ||
-        si::quant_groups(G, R, C, block_rows) >= top)
+    if (G > top || R > top || C > top || G > ((int64_t)1 << 36) / R ||
+        si::quant_blocks(G, R, C, block_rows) >= (int64_t)1 << (block_rows == 1 ? 28 : 23))
         return SI_ERR_UNSUPPORTED;
     if (!x || !codes || !scales || !aligned16(x) || !aligned16(codes)) return SI_ERR_INVALID;
     return from_hip(si::launch_quant(x, xdt, G, R, C, block_rows, codes, scales,
@@ -496,13 +504,13 @@ int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C
 }
 
 size_t si_matmul_fp8_workspace(int64_t M, int64_t N, int64_t K) {
-    if (M < 1 || N < 1 || K < 1) return 0;
+    if (M < 1 || N < 1 || K < 1 || !fp8_sizes(M, N, K)) return 0;
     return si::fp8_workspace(M, N, K);
 }
 
 int si_matmul_fp8_plan(int64_t M, int64_t N, int64_t K, si_dtype ydt, int32_t* plan) {
     if (M < 1 || N < 1 || K < 1 || !plan) return SI_ERR_INVALID;
-    if (!valid_dtype(ydt)) return SI_ERR_UNSUPPORTED;
+    if (!valid_dtype(ydt) || !fp8_sizes(M, N, K)) return SI_ERR_UNSUPPORTED;
     si::fp8_tiles_of(M, N, K, ydt, plan);
     return SI_OK;
 }
@@ -512,7 +520,7 @@ int si_matmul_fp8(const uint8_t* x, const float* x_scales, int64_t M, int64_t K,
                   size_t ws_bytes, void* hip_stream) {
     if (M < 0 || N < 1 || K < 1) return SI_ERR_INVALID;
     if (!valid_dtype(ydt)) return SI_ERR_UNSUPPORTED;
-    if (K % 16 != 0 || K > (1 << 20) || M > (1 << 24) || N > (1 << 24)) return SI_ERR_UNSUPPORTED;
+    if (K % 16 != 0 || !fp8_sizes(M, N, K)) return SI_ERR_UNSUPPORTED;
     if (M == 0) return SI_OK;
     if (!x || !x_scales || !w || !w_scales || !y) return SI_ERR_INVALID;
     if (!aligned16(x) || !aligned16(w) || !aligned16(y)) return SI_ERR_INVALID;
@@ -523,7 +531,7 @@ int si_matmul_fp8(const uint8_t* x, const float* x_scales, int64_t M, int64_t K,
 }
 
 size_t si_moe_route_workspace(int64_t T, int64_t E, int64_t d) {
-    if (T < 1 || E < 1 || d < 1) return 0;
+    if (T < 1 || E < 1 || d < 1 || !route_sizes(T, E, d)) return 0;
     return si::route_workspace(T, E, d);
 }
 

@@ -157,10 +157,8 @@ hipError_t launch(const void* x, int64_t G, int64_t R, int64_t C, int block_rows
 
 }  // namespace
 
-// work-groups of the call (its grid must stay below 2^31)
-int64_t quant_groups(int64_t G, int64_t R, int64_t C, int block_rows) {
-    const int64_t nc = (C + kBlk - 1) / kBlk;
-    return block_rows == 1 ? (G * R * nc + 15) / 16 : G * ((R + kBlk - 1) / kBlk) * nc;
+int64_t quant_blocks(int64_t G, int64_t R, int64_t C, int block_rows) {
+    return G * ((R + block_rows - 1) / block_rows) * ((C + kBlk - 1) / kBlk);
 }
 
 hipError_t launch_quant(const void* x, int xdt, int64_t G, int64_t R, int64_t C, int block_rows,

@@ -153,8 +153,8 @@ hipError_t launch_residual_rmsnorm(const void* x, int xdt, const float* y, int64
                                    float eps, void* x_out, hipStream_t s);
 
 // ---- k_quant.hip, k_fp8.hip: block-scaled 8-bit matrices ----------------------------------
-// work-groups of a quantisation (block_rows 1 or 128)
-int64_t quant_groups(int64_t G, int64_t R, int64_t C, int block_rows);
+// scale blocks of a quantisation (block_rows 1 or 128)
+int64_t quant_blocks(int64_t G, int64_t R, int64_t C, int block_rows);
 hipError_t launch_quant(const void* x, int xdt, int64_t G, int64_t R, int64_t C, int block_rows,
                         uint8_t* codes, float* scales, hipStream_t s);
 size_t fp8_workspace(int64_t M, int64_t N, int64_t K);

@@ -101,6 +101,20 @@ def test_workspace_queries(lib):  # noqa: F811
     assert lib.si_moe_layer_workspace(0, 2, 8, 64, 48, BF16, BF16, F32) == 0
 
 
+def test_queries_out_of_range(lib):  # noqa: F811
+    """Sizes past every limit are answered, not computed with: no division by a wrapped zero."""
+    plan = (ctypes.c_int32 * 3)()
+    for M, N, K in ((17, 17, 1 << 39), (1 << 40, 1 << 40, 64), (1 << 62, 1 << 62, 1 << 62),
+                    (1 << 24, 1 << 24, 64), (17, 1 << 25, 64)):
+        assert lib.si_matmul_fp8_workspace(M, N, K) == 0
+        assert lib.si_matmul_fp8_plan(M, N, K, BF16, plan) == UNSUPPORTED
+    assert lib.si_matmul_fp8_plan(1 << 20, 1 << 20, 64, BF16, plan) == OK
+    for T, E, d in ((1 << 34, 1 << 38, 64), (65536, 8, 64), (4, 1025, 64), (4, 8, 1 << 62)):
+        assert lib.si_moe_route_workspace(T, E, d) == 0
+    assert lib.si_moe_ffn_workspace(1 << 62, 1 << 62, 8, 64, 48, BF16, BF16, F32) == 0
+    assert lib.si_moe_layer_workspace(4, 2, 8, 1 << 62, 1 << 62, BF16, BF16, F32) == 0
+
+
 def test_every_tile_is_value_checked(lib):  # noqa: F811
     """The sizes of the GPU tests reach every tile of the 8-bit product, each with and without K
     chunks, for float32 and 16-bit results."""
@@ -149,6 +163,11 @@ def test_quantize_refusals(lib, mem):  # noqa: F811
     assert f(x=mem + 8) == f(codes=mem + 8) == INVALID
     assert f(R=0, x=None, codes=None, scales=None) == f(G=0, x=None) == OK
     assert f(R=1 << 31, C=1 << 20) == f(G=1 << 33, R=1 << 33) == UNSUPPORTED
+    # block counts that would wrap 64 bits, or a launch of 2^32 threads
+    assert f(G=1 << 20, R=1 << 20, C=1 << 31) == f(G=1 << 20, R=1 << 20, C=1 << 31, br=128) \
+        == UNSUPPORTED
+    assert f(R=1 << 28) == f(R=1 << 20, C=128 << 8) == UNSUPPORTED
+    assert f(R=1 << 30, br=128) == UNSUPPORTED
 
 
 def test_matmul_refusals(lib, mem):  # noqa: F811
