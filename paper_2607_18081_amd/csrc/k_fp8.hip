@@ -176,13 +176,13 @@ __global__ __launch_bounds__(kRowWaves * 64) void fp8_rows(
 //
 // What bounds it (4096 tokens, 14336 x 4096, 241 us, 2.0 PFLOP/s; with one scale a tensor the
 // library's product takes 213): the loads of a step, 64 KB a CU from the XCD's L2. Without the
-// MFMAs 255 us, without memory behind the loads 210, without the stores 226. In the order found: the
-// compiler's own waits for the loads just issued (one array a stage, 402 -> 280 us; the loop must
-// also not be left in mid-round, or the accumulators live twice and spill), lines first read one
-// step before use (touched ahead, 295 -> 271), prologue and stores of each tile (loads run on into
-// the next, 271 -> 248), the weights' scales as scalar loads (246 -> 241). A different K order in
-// each tile, three stages of 256 x 128 tiles and the next operands read before the barrier changed
-// little.
+// MFMAs 255 us, without memory behind the loads 210, without the stores 226. In the order found:
+// the compiler's own waits for the loads just issued (one array a stage, 402 -> 280 us; the loop
+// must also not be left in mid-round, or the accumulators live twice and spill), lines first read
+// one step before use (touched ahead, 295 -> 271), prologue and stores of each tile (loads run on
+// into the next, 271 -> 248), the weights' scales as scalar loads (246 -> 241). A different K order
+// in each tile, three stages of 256 x 128 tiles and the next operands read before the barrier
+// changed little.
 struct Item {
     int id;  // -1: past the last
     int tm, tn, b0, b1;

@@ -2,11 +2,11 @@
 //
 //   y[t] = sum over r < k of w[t][r] * D_e (SiLU(G_e x[t]) * (U_e x[t])),   e = ids[t][r]
 //
-// gate_up [E][2][I][d] and down [E][d][I] are read where they lie, each chosen expert once per 16 to
-// 64 of its tokens: with few tokens the time is that of streaming the chosen experts' weights, and
-// every product runs on MFMAs whose token operand is mostly padding (16 tokens a tile), which is
-// free below the weights' rate. Three kernels: gate/up with SiLU(g) * u, down, weighted sum; two for
-// one token, the router's choice included.
+// gate_up [E][2][I][d] and down [E][d][I] are read where they lie, each chosen expert once per 16
+// to 64 of its tokens: with few tokens the time is that of streaming the chosen experts' weights,
+// and every product runs on MFMAs whose token operand is mostly padding (16 tokens a tile), which
+// is free below the weights' rate. Three kernels: gate/up with SiLU(g) * u, down, weighted sum; two
+// for one token, the router's choice included.
 //
 // A pair is an entry p = t * k + r of ids. A work-group takes one expert and a tile of weight
 // rows, finds the expert's pairs by reading ids itself (no list kernel, no launch that waits for
@@ -14,8 +14,8 @@
 // for it and it adds nothing.
 //
 // Rates (weights of the experts that were chosen): 48 tokens over 8 experts of 14336 x 4096 in bf16
-// 486 us, 5.8 TB/s; 13 tokens over 64 8-bit experts of 1408 x 4096 157 us, 5.1 TB/s; one token through
-// 8 of 128 experts of 768 x 2048 25.6 us, of which three launches cost about 7.
+// 486 us, 5.8 TB/s; 13 tokens over 64 8-bit experts of 1408 x 4096 157 us, 5.1 TB/s; one token
+// through 8 of 128 experts of 768 x 2048 25.6 us, of which three launches cost about 7.
 //
 // Element types: float32, bf16, half, or e4m3 codes with a float32 scale for each 128 x 128
 // weights. Codes become the 16-bit type of x (exactly); a scale block's products are summed in
@@ -85,8 +85,9 @@ struct Core<XT, true> {
 // the work-group calls it. by_pair: the grid's slot is a pair, and the work-group serves that
 // pair's expert only if no earlier pair has it (else 0); otherwise the slot is the expert.
 template <int W>
-__device__ __forceinline__ int expert_pairs(const int32_t* __restrict__ ids, int npairs, int E, int slot,
-                            int by_pair, int& e, uint16_t* list, int* cnt) {
+__device__ __forceinline__ int expert_pairs(const int32_t* __restrict__ ids, int npairs, int E,
+                                            int slot, int by_pair, int& e, uint16_t* list,
+                                            int* cnt) {
     const int lane = threadIdx.x & 63;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     e = slot;
@@ -419,7 +420,8 @@ __device__ __forceinline__ void gate_up_pass(
     constexpr int NQ = NR * NT;
     if constexpr (WK == 1) {
 #pragma unroll
-        for (int q = 0; q < NQ; ++q) finish(q, acc[2 * (q / NT)][q % NT], acc[2 * (q / NT) + 1][q % NT]);
+        for (int q = 0; q < NQ; ++q)
+            finish(q, acc[2 * (q / NT)][q % NT], acc[2 * (q / NT) + 1][q % NT]);
     } else {
         __syncthreads();  // the rings are done with
 #pragma unroll
@@ -461,7 +463,8 @@ __global__ __launch_bounds__(WK * 64) void moe_gate_up(
     const int wk = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
     const uint8_t* gu = gate_up + (int64_t)e * 2 * I * d * WB;
-    const float* gs = FP8 ? scales + (int64_t)e * 2 * ((I + 127) / 128) * ((d + 127) / 128) : nullptr;
+    const int nb = (I + 127) / 128;
+    const float* gs = FP8 ? scales + (int64_t)e * 2 * nb * ((d + 127) / 128) : nullptr;
     const int n0 = blockIdx.x * 16 * NR;
     const int64_t plane = (int64_t)npairs * I;
     char* const ring = rings + wk * RING;
@@ -469,12 +472,16 @@ __global__ __launch_bounds__(WK * 64) void moe_gate_up(
     const int64_t xb = T * d * (int64_t)sizeof(XT);
     for (int c = 0; c < m; c += 16 * MT) {
         const int mc = min(m - c, 16 * MT);
+        auto pass = [&](auto tiles) {
+            gate_up_pass<XT, FP8, RING, WK, NR, decltype(tiles)::value>(
+                x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, wk, ring, red);
+        };
         if (mc <= 16)
-            gate_up_pass<XT, FP8, RING, WK, NR, 1>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, wk, ring, red);
+            pass(std::integral_constant<int, 1>());
         else if (MT < 4 || mc <= 32)
-            gate_up_pass<XT, FP8, RING, WK, NR, (MT < 2 ? MT : 2)>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, wk, ring, red);
+            pass(std::integral_constant<int, MT < 2 ? MT : 2>());
         else
-            gate_up_pass<XT, FP8, RING, WK, NR, MT>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane, parts, wk, ring, red);
+            pass(std::integral_constant<int, MT>());
     }
 }
 
@@ -592,12 +599,16 @@ __global__ __launch_bounds__(WK * WR * 64) void moe_down(
     f32x4_t* const red = reinterpret_cast<f32x4_t*>(rings + wr * WK * RING);
     for (int c = 0; c < m; c += 16 * MT) {
         const int mc = min(m - c, 16 * MT);
+        auto pass = [&](auto tiles) {
+            down_pass<HT, FP8, PARTS, RING, WK, RT, decltype(tiles)::value>(
+                H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
+        };
         if (mc <= 16)
-            down_pass<HT, FP8, PARTS, RING, WK, RT, 1>(H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
+            pass(std::integral_constant<int, 1>());
         else if (MT < 4 || mc <= 32)
-            down_pass<HT, FP8, PARTS, RING, WK, RT, (MT < 2 ? MT : 2)>(H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
+            pass(std::integral_constant<int, MT < 2 ? MT : 2>());
         else
-            down_pass<HT, FP8, PARTS, RING, WK, RT, MT>(H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
+            pass(std::integral_constant<int, MT>());
     }
 }
 
@@ -788,8 +799,8 @@ __global__ __launch_bounds__(256) void moe_gate_up_one(
     f32x4_t acc[RT][1];
 #pragma unroll
     for (int q = 0; q < RT; ++q) acc[q][0] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    lines_one<XT, FP8, RT, 1, D>(acc, wr, woff, rb, lds_addr(hs) + (FP8 ? 32 * g : 16 * g), 0, sc, l0,
-                                 l1, rings + wave * D * 2 * RT * 1024, [&]() {
+    lines_one<XT, FP8, RT, 1, D>(acc, wr, woff, rb, lds_addr(hs) + (FP8 ? 32 * g : 16 * g), 0, sc,
+                                 l0, l1, rings + wave * D * 2 * RT * 1024, [&]() {
                                      // every wave's part of x has landed (the weights may fly)
                                      wait_vm_lds<D * 2 * RT>();
                                      wg_barrier();
@@ -837,8 +848,8 @@ __global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
     const int rb = I * WB, hb = I * (int)sizeof(HT), pitch = one_pitch(I, sizeof(HT));
     const int nl = (rb + kLine - 1) / kLine, per = (nl + kc - 1) / kc;
     // row r of part p of h at (p k + r) pitch
-    stage_rows<kOneWaves>(make_rsrc(H, (int64_t)PARTS * k * I * sizeof(HT)), PARTS * k, hb, pitch, hs,
-                          wave, lane);
+    stage_rows<kOneWaves>(make_rsrc(H, (int64_t)PARTS * k * I * sizeof(HT)), PARTS * k, hb, pitch,
+                          hs, wave, lane);
     const int woff[1][2] = {{c0 + lr < d ? (c0 + lr) * rb : kOOB,
                              c0 + 8 + lr < d ? (c0 + 8 + lr) * rb : kOOB}};
     bool ready = false;
@@ -943,9 +954,9 @@ void sum(const Args& a, YT* y) {
 }
 
 // Lines of a weight row from which it counts as long: more waves then share one row group, so that
-// fewer work-groups take more of a row at a time (48 tokens over 8 experts of 14336 x 4096: gate and
-// up by 4 waves 525 us a layer, by 2 542; down by 2 518, by 1 541; 13 tokens over 8-bit experts with
-// rows of 1408, 11 lines: down by 1 wave 159, by 2 187).
+// fewer work-groups take more of a row at a time (48 tokens over 8 experts of 14336 x 4096: gate
+// and up by 4 waves 525 us a layer, by 2 542; down by 2 518, by 1 541; 13 tokens over 8-bit experts
+// with rows of 1408, 11 lines: down by 1 wave 159, by 2 187).
 constexpr int kLongRow = 64;
 
 // Pairs an expert from which the tokens' operand, which every wave loads for its own rows, weighs
@@ -968,7 +979,8 @@ void experts(const Args& a) {
     const size_t lds = ((size_t)np * sizeof(uint16_t) + 15) / 16 * 16;
     const int gl = (int)((a.d * (FP8 ? 1 : (int)sizeof(XT)) + kLine - 1) / kLine);
     const int dl = (int)((a.I * (FP8 ? 1 : (int)sizeof(HT)) + kLine - 1) / kLine);
-    const bool many = sizeof(XT) == 2 && (int64_t)np >= kManyPairs * a.E;
+    constexpr bool kMany = sizeof(XT) == 2;
+    const bool many = kMany && (int64_t)np >= kManyPairs * a.E;
     const XT* x = static_cast<const XT*>(a.x);
     const int64_t xlds = one_pitch(a.d, sizeof(XT));
     if (a.T == 1 && xlds <= kOneX) {
@@ -979,21 +991,30 @@ void experts(const Args& a) {
                 H, a.p.parts);
         else
             moe_gate_up_one<XT, FP8, false><<<grid, 256, (size_t)xlds, a.s>>>(
-                x, (int)a.d, Choice{}, a.ids, a.w, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, H,
-                a.p.parts);
+                x, (int)a.d, Choice{}, a.ids, a.w, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I,
+                H, a.p.parts);
     } else {
         auto gate = [&](auto kernel, int rows, int threads) {
             kernel<<<dim3((unsigned)((a.I + rows - 1) / rows), slots), threads, lds, a.s>>>(
-                x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I, by_pair,
-                H, a.p.parts);
+                x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I,
+                by_pair, H, a.p.parts);
         };
-        if (many)
-            gate(moe_gate_up<XT, FP8, 48 * 1024, 2, 2>, 32, 128);
-        else if (gl >= kLongRow)
+        if (many) {
+            if constexpr (kMany) gate(moe_gate_up<XT, FP8, 48 * 1024, 2, 2>, 32, 128);
+        } else if (gl >= kLongRow) {
             gate(moe_gate_up<XT, FP8, 16 * 1024, 4, 1>, 16, 256);
-        else
+        } else {
             gate(moe_gate_up<XT, FP8, 24 * 1024, 2, 1>, 16, 128);
+        }
     }
+    // f(y) with y's type: bf16 parts number 3 for a float32 y and 2 for one of 16 bits
+    auto to_y = [&](auto f) {
+        constexpr bool kF32 = PARTS != 2 || std::is_same<HT, f16_t>::value;
+        if constexpr (PARTS == 2) {
+            if (!kF32 || a.ydt != 0) return f(static_cast<XT*>(a.y));
+        }
+        if constexpr (kF32) f(static_cast<float*>(a.y));
+    };
     const int64_t hlds = (int64_t)PARTS * a.k * one_pitch(a.I, sizeof(HT));
     if (a.T == 1 && hlds <= kOneH) {
         // one token: as many runs of K as keep the waves busy
@@ -1004,26 +1025,21 @@ void experts(const Args& a) {
             moe_down_one<HT, FP8, PARTS, YT><<<grid, kOneWaves * 64, (size_t)hlds, a.s>>>(
                 H, (int)a.d, a.ids, a.w, (int)a.k, kc, a.down, a.dns, (int)a.E, (int)a.I, y);
         };
-        if (a.ydt == 0)
-            one(static_cast<float*>(a.y));
-        else if constexpr (sizeof(XT) == 2)
-            one(static_cast<XT*>(a.y));
+        to_y(one);
         return;
     }
     auto down = [&](auto kernel, int rows, int threads) {
         kernel<<<dim3((unsigned)((a.d + rows - 1) / rows), slots), threads, lds, a.s>>>(
             H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
     };
-    if (many)
-        down(moe_down<HT, FP8, PARTS, 48 * 1024, 1, 2, 4>, 128, 128);
-    else if (dl >= kLongRow)
+    if (many) {
+        if constexpr (kMany) down(moe_down<HT, FP8, PARTS, 48 * 1024, 1, 2, 4>, 128, 128);
+    } else if (dl >= kLongRow) {
         down(moe_down<HT, FP8, PARTS, 24 * 1024, 2, 2, 2>, 64, 256);
-    else
+    } else {
         down(moe_down<HT, FP8, PARTS, 24 * 1024, 1, 2, 2>, 64, 128);
-    if (a.ydt == 0)
-        sum(a, static_cast<float*>(a.y));
-    else if constexpr (sizeof(XT) == 2)
-        sum(a, static_cast<XT*>(a.y));
+    }
+    to_y([&](auto* y) { sum(a, y); });
 }
 
 }  // namespace

@@ -43,20 +43,22 @@ struct Mfma<f16_t> {
 
 // 8 e4m3 codes as bf16 (every e4m3 value is a bf16 value)
 __device__ __forceinline__ V16 e4m3_to_bf16(uint32_t lo, uint32_t hi) {
+    auto two = [](auto v) { return __builtin_bit_cast(uint32_t, v); };
     V16 o;
-    o.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
-    o.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
-    o.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
-    o.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
+    o.w[0] = two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false));
+    o.w[1] = two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true));
+    o.w[2] = two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false));
+    o.w[3] = two(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true));
     return o;
 }
 // and as half (every e4m3 value is a half value too)
 __device__ __forceinline__ V16 e4m3_to_f16(uint32_t lo, uint32_t hi) {
+    auto two = [](auto v) { return __builtin_bit_cast(uint32_t, v); };
     V16 o;
-    o.w[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
-    o.w[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
-    o.w[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
-    o.w[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+    o.w[0] = two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+    o.w[1] = two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+    o.w[2] = two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+    o.w[3] = two(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
     return o;
 }
 

@@ -121,12 +121,17 @@ def test_every_tile_is_value_checked(lib):  # noqa: F811
     import paper_2607_18081_amd as si
     from tests.test_gpu_fp8 import LARGE, NAMES
     seen = {(dt == "f32", *si.matmul_fp8_plan(M, N, K, NAMES[dt])) for M, N, K, dt in LARGE}
+    chunks = {(256, 256): (1, 2, 4), (256, 128): (1, 2, 4), (128, 128): (1, 2, 4),
+              (128, 64): (1, 2, 4), (64, 64): (1, 2, 4)}
     for exact in (False, True):
-        tiles = [(256, 256), (256, 128), (128, 128), (128, 64), (64, 64)][exact:]
-        for t in tiles:
-            assert any(s[:3] == (exact, *t) for s in seen), (exact, t)
-        assert any(s[0] == exact and s[3] > 1 for s in seen)
-    assert {s[1:3] for s in seen if s[3] > 1} >= {(256, 256), (256, 128), (128, 128), (64, 64)}
+        for t in list(chunks)[exact:]:
+            for ks in chunks[t]:
+                assert (exact, *t, ks) in seen, (exact, t, ks)
+    for M in (17, 33, 64, 100, 130, 200, 260, 384, 700, 1500):      # no other is reached
+        for N in range(64, 6000, 64):
+            for K in (400, 2560, 5120, 10240, 14336):
+                for dt in ("bf16", "f32"):
+                    assert (dt == "f32", *si.matmul_fp8_plan(M, N, K, NAMES[dt])) in seen
     assert si.matmul_fp8_plan(1, 4096, 4096)[0] == 0
     for M in (1, 5, 17, 64, 200, 1000, 5000):
         for N in (1, 100, 3000, 20000):

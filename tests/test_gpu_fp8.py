@@ -124,6 +124,10 @@ LARGE = [
     (1500, 5000, 5264, "bf16"), (250, 3400, 400, "bf16"), (250, 3400, 400, "f32"),
     (60, 4000, 4112, "f16"),
     (60, 4000, 2064, "f32"), (9, 10500, 272, "bf16"), (9, 10500, 400, "f32"),
+    (17, 200, 5136, "f32"), (100, 3131, 10256, "bf16"), (100, 3131, 10256, "f32"),
+    (130, 3131, 10256, "bf16"), (130, 3131, 10256, "f32"), (130, 4283, 5136, "bf16"),
+    (130, 4283, 5136, "f32"), (1001, 4000, 5264, "f32"), (900, 3333, 10256, "bf16"),
+    (260, 4155, 10256, "bf16"), (260, 4155, 10256, "f32"),
 ]
 NAMES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
