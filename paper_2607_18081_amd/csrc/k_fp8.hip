@@ -449,11 +449,18 @@ __global__ __launch_bounds__(256) void fp8_sum(const float* __restrict__ part, i
     }
 }
 
-// Tiles by number, the largest first: rows x tokens, stages, work-groups that fit a CU
+// Tiles by number, the largest first: rows x tokens; microseconds that a CU spends on a K step of
+// one (with codes as they are, and widened) and on starting and storing one. The 256 x 256 tile's
+// registers do not hold widened codes.
 struct Tile {
     int bn, bm;
+    float step, wide, start;
 };
-constexpr Tile kTiles[] = {{256, 256}, {256, 128}, {128, 128}, {128, 64}, {64, 64}};
+constexpr Tile kTiles[] = {{256, 256, 1.7f, 0.0f, 1.9f},
+                           {256, 128, 0.93f, 1.86f, 3.5f},
+                           {128, 128, 0.73f, 1.02f, 0.57f},
+                           {128, 64, 0.37f, 0.67f, 1.5f},
+                           {64, 64, 0.24f, 0.46f, 0.2f}};
 constexpr int kNumTiles = 5;
 
 struct Fp8Plan {
@@ -462,36 +469,42 @@ struct Fp8Plan {
     int per;   // blocks a chunk
 };
 
-// Weights of few rows and up to 16 tokens: fp8_rows. From 160 tiles of 64 rows on the 64 x 64 tile
-// streams them as fast and reads x once for 64 rows instead of 16 (14336 x 4096: one token 15.1 us
-// by rows and 14.4 by tiles, 16 tokens 22.5 and 15.3; 4096 x 4096, 64 tiles: 6.1 and 10.4, 7.4 and
-// 10.9); a float32 result spends its tiles' time on widening codes of padding, so up to 4 tokens
-// stay with the rows (15.3 and 18.6).
-// Otherwise the largest tile of which there are about as many as CUs, K split in up to 4 chunks of
-// at least 20 blocks for it (partial sums cost as much as a few blocks): 14336 x 4096, 1024 tokens
-// 68 us by 256 x 256, 95 by 256 x 128 or 128 x 128; 512 tokens 51 us by 256 x 128, 66 by 256 x 256
-// and 60 with two chunks of 16 blocks; 4096 x 11008, 512 tokens 46.9 us by 128 x 128 in two chunks,
-// 54 by 128 x 64. The smallest tile takes any split that fills the chip: 4096 x 11008, 32 tokens
-// 25 us in one chunk, 14.8 in four.
-// The 256 x 256 tile's registers do not hold widened codes (EXACT).
+// The variant of the least estimated time: the launch, the rounds of work-groups over 256 CUs (but
+// no less than the weights' bytes take), and the partial sums of a split K. Its constants are a fit
+// to every tile with 1, 2 and 4 chunks and the rows, at 1 to 4096 tokens, 256 to 28672 rows and 512
+// to 14336 columns (11000 times, off by 11% in the mean); the variants it takes are 1.5% slower than
+// the best of each size in the mean, where "the largest tile that fills the chip" lost 7%. Some of
+// them, in us:
+//   13 tokens, 11008 x 4096    64 x 64 9.9, in two chunks 13.0, rows 14.8
+//   13 tokens, 4096 x 14336    64 x 64 23.8, in two chunks 16.0, in four 14.3
+//    5 tokens, 14336 x 14336   64 x 64 39, 256 x 256 in four chunks 64
+//  300 tokens, 11008 x 7168 (float32 y)  128 x 64 68, 256 x 128 in two chunks 114
+//  128 tokens, 11008 x 7168    128 x 64 25.7, in two chunks 40.3
 Fp8Plan fp8_plan(int64_t M, int64_t N, int64_t K, bool exact) {
     const int kb = (int)((K + kBlk - 1) / kBlk);
-    if (M <= 16 && ((N + 63) / 64 < 160 || (exact && M <= 4))) return {-1, 1, kb};
-    constexpr int64_t kFull = 200;
+    constexpr double kCU = 256;
+    Fp8Plan best{-1, 1, kb};
+    double least = HUGE_VAL;
+    if (M <= 16) {
+        const double n = (double)((N + 15) / 16);
+        least = 3.6 + kb / 8.0 * (0.56 + n / kCU * (0.47 + 0.032 * (double)M));
+    }
     for (int t = exact ? 1 : 0; t < kNumTiles; ++t) {
-        const int64_t n = ((N + kTiles[t].bn - 1) / kTiles[t].bn) *
-                          ((M + kTiles[t].bm - 1) / kTiles[t].bm);
-        const bool smallest = t + 1 == kNumTiles;
-        for (int ks = 1; ks <= 4; ks *= 2) {
-            if (ks > 1 && kb / ks < (smallest ? 8 : 20)) break;
-            const bool most = smallest && (ks == 4 || kb / (2 * ks) < 8);
-            if (n * ks >= kFull || most) {
-                const int per = (kb + ks - 1) / ks;
-                return {t, (kb + per - 1) / per, per};
+        const Tile& c = kTiles[t];
+        const int64_t n = ((N + c.bn - 1) / c.bn) * ((M + c.bm - 1) / c.bm);
+        for (int ks = 1; ks <= 4 && (ks == 1 || kb >= 4 * ks); ks *= 2) {
+            const int per = (kb + ks - 1) / ks, chunks = (kb + per - 1) / per;
+            const double rounds = ceil((double)(n * chunks) / kCU);
+            double us = rounds * (per * (double)(exact ? c.wide : c.step) + c.start);
+            us = 4.3 + fmax(us, (double)N * (double)K / 7.4e6);
+            if (chunks > 1) us += 3.1 + (double)chunks * (double)M * (double)N * 8.0 / 4.8e6;
+            if (us < least) {
+                least = us;
+                best = Fp8Plan{t, chunks, per};
             }
         }
     }
-    return {kNumTiles - 1, 1, kb};
+    return best;
 }
 
 template <int T, int WN, int WM, int S, typename YT, bool EXACT>

@@ -116,22 +116,20 @@ def test_queries_out_of_range(lib):  # noqa: F811
 
 
 def test_every_tile_is_value_checked(lib):  # noqa: F811
-    """The sizes of the GPU tests reach every tile of the 8-bit product, each with and without K
-    chunks, for float32 and 16-bit results."""
+    """The sizes of the GPU tests reach every tile of the 8-bit product, for float32 and 16-bit
+    results, with K whole and in chunks."""
     import paper_2607_18081_amd as si
     from tests.test_gpu_fp8 import LARGE, NAMES
     seen = {(dt == "f32", *si.matmul_fp8_plan(M, N, K, NAMES[dt])) for M, N, K, dt in LARGE}
-    chunks = {(256, 256): (1, 2, 4), (256, 128): (1, 2, 4), (128, 128): (1, 2, 4),
-              (128, 64): (1, 2, 4), (64, 64): (1, 2, 4)}
+    seen = {(*s[:3], s[3] > 1) for s in seen}
     for exact in (False, True):
-        for t in list(chunks)[exact:]:
-            for ks in chunks[t]:
-                assert (exact, *t, ks) in seen, (exact, t, ks)
-    for M in (17, 33, 64, 100, 130, 200, 260, 384, 700, 1500):      # no other is reached
-        for N in range(64, 6000, 64):
-            for K in (400, 2560, 5120, 10240, 14336):
-                for dt in ("bf16", "f32"):
-                    assert (dt == "f32", *si.matmul_fp8_plan(M, N, K, NAMES[dt])) in seen
+        for t in [(256, 256), (256, 128), (128, 128), (128, 64), (64, 64)][exact:]:
+            assert {(exact, *t, False), (exact, *t, True)} <= seen, (exact, t)
+    assert not any(s[:2] == (True, 256) and s[2] == 256 for s in seen)
+    for M in (17, 64, 100, 260, 700, 1500, 4096):
+        for N in range(64, 20000, 320):
+            for K in (400, 2560, 10240, 28672):
+                assert si.matmul_fp8_plan(M, N, K, torch.float32)[:2] != (256, 256)
     assert si.matmul_fp8_plan(1, 4096, 4096)[0] == 0
     for M in (1, 5, 17, 64, 200, 1000, 5000):
         for N in (1, 100, 3000, 20000):

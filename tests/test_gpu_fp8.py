@@ -128,6 +128,10 @@ LARGE = [
     (130, 3131, 10256, "bf16"), (130, 3131, 10256, "f32"), (130, 4283, 5136, "bf16"),
     (130, 4283, 5136, "f32"), (1001, 4000, 5264, "f32"), (900, 3333, 10256, "bf16"),
     (260, 4155, 10256, "bf16"), (260, 4155, 10256, "f32"),
+    (817, 601, 14080, "bf16"), (452, 515, 9536, "bf16"), (66, 6461, 28048, "bf16"),
+    (961, 1030, 11216, "bf16"), (1190, 1733, 16896, "f16"), (18, 258, 1728, "f32"),
+    (1308, 722, 7824, "f32"), (1856, 2312, 1680, "f32"), (1276, 790, 17712, "f32"),
+    (1748, 1769, 23488, "f32"),
 ]
 NAMES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
 
