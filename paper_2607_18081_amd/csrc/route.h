@@ -76,8 +76,19 @@ __device__ __forceinline__ void choose_experts(const Choice& a, int t, bool publ
     }
     const bool mine = i < E;
     double z = 0.0;
-    if (mine)
-        for (int q = 0; q < a.KS; ++q) z += a.part[((int64_t)q * a.T + t) * E + i];
+    if (mine) {
+        // (four loads at once: one after the other they cost a memory latency each)
+        const double* part = a.part + (int64_t)t * E + i;
+        const int64_t plane = (int64_t)a.T * E;
+        for (int q = 0; q < a.KS; q += 4) {
+            double v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = part[min(q + j, a.KS - 1) * plane];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (q + j < a.KS) z += v[j];
+        }
+    }
     // the score of a softmax by its logit alone, until the chosen are known
     const bool late = !a.sigmoid && a.renorm && !a.bias;
     double p = z;
