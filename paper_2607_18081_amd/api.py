@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 from dataclasses import dataclass
+from functools import lru_cache
 
 import torch
 
@@ -480,16 +481,24 @@ def _blocks(n: int) -> int:
 
 
 def _need(t, name: str, dev: torch.device, dtype, shape) -> None:
-    """t is a contiguous tensor of that type (or one of those) and shape (a tuple) on that
-    device. The checks that pass cost what the attributes do: a call is a few microseconds."""
-    if t.dtype is not dtype and t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
+    """t is a contiguous tensor of that type (one of those, if a tuple) and shape (a tuple) on that
+    device. A check that passes costs what the attributes do: a call is a few microseconds."""
+    if t.shape == shape and t.device == dev and t.is_contiguous() and \
+            (t.dtype is dtype or dtype.__class__ is tuple and t.dtype in dtype):
+        return
+    if t.dtype not in (dtype if isinstance(dtype, tuple) else (dtype,)):
         raise ValueError(f"{name} must be {dtype}, not {t.dtype}")
     if t.shape != shape:
         raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
     if t.device != dev:
         raise ValueError(f"{name} must be on {dev}")
-    if not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
+    raise ValueError(f"{name} must be contiguous")
+
+
+# Workspace bytes by sizes alone (a query costs 0.6 us a call, its remembered answer 0.1)
+@lru_cache(maxsize=1024)
+def _bytes(query: str, *sizes: int) -> int:
+    return getattr(load(), query)(*sizes)
 
 
 def _space(workspace, nbytes: int, dev: torch.device) -> torch.Tensor:
@@ -519,8 +528,8 @@ def _run(fn, where: str, dev: torch.device, *args) -> None:
 
 
 def _p(t):
-    """Address of a tensor already known to be contiguous (None: no tensor, or an empty one)."""
-    return (t.data_ptr() or None) if t is not None else None
+    """Address of an optional tensor already known to be contiguous."""
+    return t.data_ptr() if t is not None else None
 
 
 def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | None = None,
@@ -547,7 +556,7 @@ def quantize_fp8(x: torch.Tensor, block_rows: int = 1, codes: torch.Tensor | Non
     else:
         _need(scales, "scales", dev, torch.float32, sshape)
     _run(load().si_quantize_fp8, "si_quantize_fp8", dev, _ptr(x), _dt(x), G, R, C, block_rows,
-         _p(codes), _p(scales))
+         codes.data_ptr(), scales.data_ptr())
     return codes, scales
 
 
@@ -578,10 +587,11 @@ def matmul_fp8(x: torch.Tensor, x_scales: torch.Tensor, w: torch.Tensor, w_scale
     else:
         _need(out, "out", dev, out_dtype, (M, N))
     lib = load()
-    need = lib.si_matmul_fp8_workspace(M, N, K)
+    need = _bytes("si_matmul_fp8_workspace", M, N, K)
     ws = _space(workspace, need, dev) if need else None
-    _run(lib.si_matmul_fp8, "si_matmul_fp8", dev, _p(x), _p(x_scales), M, K, _p(w), _p(w_scales),
-         N, _p(out), _dt(out), _p(ws), ws.numel() if need else 0)
+    _run(lib.si_matmul_fp8, "si_matmul_fp8", dev, x.data_ptr(), x_scales.data_ptr(), M, K,
+         w.data_ptr(), w_scales.data_ptr(), N, out.data_ptr(), _dt(out), _p(ws),
+         ws.numel() if need else 0)
     return out
 
 
@@ -650,9 +660,10 @@ def moe_route(x: torch.Tensor, w_router: torch.Tensor, k: int, bias: torch.Tenso
     dev, T, d, E, mode, ids, weights = _route_args(x, w_router, k, bias, score, renorm, n_valid,
                                                    ids, weights)
     lib = load()
-    ws = _space(workspace, lib.si_moe_route_workspace(T, E, d), dev)
-    _run(lib.si_moe_route, "si_moe_route", dev, _p(x), _dt(x), T, d, _p(w_router), _dt(w_router),
-         E, _p(bias), k, mode, float(scale), _p(n_valid), _p(ids), _p(weights), _p(ws), ws.numel())
+    ws = _space(workspace, _bytes("si_moe_route_workspace", T, E, d), dev)
+    _run(lib.si_moe_route, "si_moe_route", dev, x.data_ptr(), _dt(x), T, d, w_router.data_ptr(),
+         _dt(w_router), E, _p(bias), k, mode, float(scale), _p(n_valid), ids.data_ptr(),
+         weights.data_ptr(), ws.data_ptr(), ws.numel())
     return ids, weights
 
 
@@ -673,9 +684,10 @@ def moe_ffn(x: torch.Tensor, ids: torch.Tensor, weights: torch.Tensor, gate_up: 
     _need(weights, "weights", dev, torch.float32, (T, k))
     E, inter, wdt, y = _expert_args(x, gate_up, down, gate_up_scales, down_scales, out_dtype, y)
     lib, xdt, ydt = load(), _dt(x), _dt(y)
-    ws = _space(workspace, lib.si_moe_ffn_workspace(T, k, E, d, inter, xdt, wdt, ydt), dev)
-    _run(lib.si_moe_ffn, "si_moe_ffn", dev, _p(x), xdt, T, d, _p(ids), _p(weights), k, _p(gate_up),
-         _p(gate_up_scales), _p(down), _p(down_scales), E, inter, wdt, _p(y), ydt, _p(ws),
+    ws = _space(workspace, _bytes("si_moe_ffn_workspace", T, k, E, d, inter, xdt, wdt, ydt), dev)
+    _run(lib.si_moe_ffn, "si_moe_ffn", dev, x.data_ptr(), xdt, T, d, ids.data_ptr(),
+         weights.data_ptr(), k, gate_up.data_ptr(), _p(gate_up_scales), down.data_ptr(),
+         _p(down_scales), E, inter, wdt, y.data_ptr(), ydt, ws.data_ptr(),
          ws.numel())
     return y
 
@@ -695,8 +707,9 @@ def moe_layer(x: torch.Tensor, w_router: torch.Tensor, gate_up: torch.Tensor, do
     if En != E:
         raise ValueError("w_router and gate_up must have one number of experts")
     lib, xdt, ydt = load(), _dt(x), _dt(y)
-    ws = _space(workspace, lib.si_moe_layer_workspace(T, k, E, d, inter, xdt, wdt, ydt), dev)
-    _run(lib.si_moe_layer, "si_moe_layer", dev, _p(x), xdt, T, d, _p(w_router), _dt(w_router),
-         _p(bias), k, mode, float(scale), _p(n_valid), _p(gate_up), _p(gate_up_scales), _p(down),
-         _p(down_scales), E, inter, wdt, _p(ids), _p(weights), _p(y), ydt, _p(ws), ws.numel())
+    ws = _space(workspace, _bytes("si_moe_layer_workspace", T, k, E, d, inter, xdt, wdt, ydt), dev)
+    _run(lib.si_moe_layer, "si_moe_layer", dev, x.data_ptr(), xdt, T, d, w_router.data_ptr(),
+         _dt(w_router), _p(bias), k, mode, float(scale), _p(n_valid), gate_up.data_ptr(),
+         _p(gate_up_scales), down.data_ptr(), _p(down_scales), E, inter, wdt, ids.data_ptr(),
+         weights.data_ptr(), y.data_ptr(), ydt, ws.data_ptr(), ws.numel())
     return y, ids, weights
