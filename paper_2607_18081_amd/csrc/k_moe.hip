@@ -6,7 +6,8 @@
 // to 64 of its tokens: with few tokens the time is that of streaming the chosen experts' weights,
 // and every product runs on MFMAs whose token operand is mostly padding (16 tokens a tile), which
 // is free below the weights' rate. Three kernels: gate/up with SiLU(g) * u, down, weighted sum; two
-// for one token, the router's choice included.
+// for one token, the router's choice included; two others for many tokens an expert, whose waves
+// share the tokens' operand.
 //
 // A pair is an entry p = t * k + r of ids. A work-group takes one expert and a tile of weight
 // rows, finds the expert's pairs by reading ids itself (no list kernel, no launch that waits for
@@ -166,7 +167,58 @@ constexpr int line_loads() {
     return 2 * RT + 2 * NT * PARTS * (FP8 ? 2 : 1);
 }
 
-// acc[r][n] += the product of RT row tiles and NT token tiles over the lines [l0, l1).
+// acc += the products of one line: operands a of the row tiles, b of the token tiles (by tile, part
+// and, for codes, 128 bytes of columns), scales sc[r][l]
+template <typename XT, bool FP8, int RT, int NT, int PARTS, int SUMS>
+__device__ __forceinline__ void line_product(f32x4_t (&acc)[SUMS][RT][NT], const V16 (&a)[RT][2],
+                                             const V16 (&b)[NT * PARTS * Core<XT, FP8>::XC][2],
+                                             const float* const (&sc)[RT], int l) {
+    using C = Core<XT, FP8>;
+    constexpr int XC = C::XC;
+    f32x4_t blk[SUMS][RT][NT];
+    if (FP8) {
+#pragma unroll
+        for (int q = 0; q < SUMS; ++q)
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) blk[q][r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            typename C::vec w[XC];
+            C::widen(a[r][h], w);
+#pragma unroll
+            for (int c = 0; c < XC; ++c)
+#pragma unroll
+                for (int p = 0; p < PARTS; ++p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        f32x4_t& t = FP8 ? blk[p % SUMS][r][n] : acc[p % SUMS][r][n];
+                        t = C::mma(w[c],
+                                   XC == 1 ? b[n * PARTS + p][h]
+                                           : b[(n * PARTS + p) * XC + h * (XC - 1)][c], t);
+                    }
+        }
+    if (FP8) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const float f = sc[r][l];
+#pragma unroll
+            for (int q = 0; q < SUMS; ++q)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        acc[q][r][n][e] = fmaf(f, blk[q][r][n][e], acc[q][r][n][e]);
+        }
+    }
+}
+
+// acc[q][r][n] += the product of RT row tiles and NT token tiles over the lines [l0, l1): one total
+// for all parts, or (half, whose parts differ in weight) one for each, SUMS = PARTS.
 //   wr, woff[r]   the expert's weights and the byte offset of row lane / 8 of tile r, in woff[r][1]
 //                 that of row lane / 8 + 8 (kOOB: no such row); rb the bytes of a row
 //   xr, xoff[n]   the same for the token operand (PARTS planes, `plane` bytes apart), xb its bytes
@@ -176,8 +228,8 @@ constexpr int line_loads() {
 // row r lies at c ^ (r % 8), so that the 16-row reads do not conflict. Loads straight into
 // registers in the operand's shape, 64 bytes of 16 rows each, streamed at 3.4 to 4.4 TB/s. Lane
 // (i, g) takes chunks g and 4 + g of row i.
-template <typename XT, bool FP8, int RT, int NT, int PARTS, int D, int POL>
-__device__ __forceinline__ void lines(f32x4_t (&acc)[RT][NT], __amdgpu_buffer_rsrc_t wr,
+template <typename XT, bool FP8, int RT, int NT, int PARTS, int SUMS, int D>
+__device__ __forceinline__ void lines(f32x4_t (&acc)[SUMS][RT][NT], __amdgpu_buffer_rsrc_t wr,
                                       const int (&woff)[RT][2], int rb, __amdgpu_buffer_rsrc_t xr,
                                       const int (&xoff)[NT][2], int xb, int plane,
                                       const float* const (&sc)[RT], int l0, int l1, char* ring) {
@@ -195,8 +247,9 @@ __device__ __forceinline__ void lines(f32x4_t (&acc)[RT][NT], __amdgpu_buffer_rs
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                load_lds16<POL>(wr, at + (2 * r + h) * 1024,
-                                (in & (woff[r][h] >= 0)) ? woff[r][h] + lcol : kOOB, l * kLine);
+                load_lds16<kNonTemporal>(wr, at + (2 * r + h) * 1024,
+                                         (in & (woff[r][h] >= 0)) ? woff[r][h] + lcol : kOOB,
+                                         l * kLine);
 #pragma unroll
         for (int c = 0; c < XC; ++c) {
             const int o = (l * XC + c) * kLine;
@@ -229,42 +282,7 @@ __device__ __forceinline__ void lines(f32x4_t (&acc)[RT][NT], __amdgpu_buffer_rs
         lds_tiles<NT * PARTS * XC, 2048 * RT>(x0 + at, x1 + at, b);
         load(l + D, ring + at);
         slot = slot + 1 == D ? 0 : slot + 1;
-        f32x4_t blk[RT][NT];
-        if (FP8) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) blk[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                typename C::vec w[XC];
-                C::widen(a[r][h], w);
-#pragma unroll
-                for (int c = 0; c < XC; ++c)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n)
-#pragma unroll
-                        for (int p = 0; p < PARTS; ++p) {
-                            f32x4_t& t = FP8 ? blk[r][n] : acc[r][n];
-                            t = C::mma(w[c],
-                                       XC == 1 ? b[n * PARTS + p][h]
-                                               : b[(n * PARTS + p) * XC + h * (XC - 1)][c], t);
-                        }
-            }
-        if (FP8) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const float s = sc[r][l];
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[r][n][e] = fmaf(s, blk[r][n][e], acc[r][n][e]);
-            }
-        }
+        line_product<XT, FP8, RT, NT, PARTS, SUMS>(acc, a, b, sc, l);
     }
     wait_vm_lds<0>();  // the ring is free again
 }
@@ -398,13 +416,14 @@ __device__ __forceinline__ void gate_up_pass(
                     : nullptr;
     int l0, l1;
     wave_lines<WK>(nl, wk, l0, l1);
-    f32x4_t acc[RT][NT];
+    f32x4_t sums[1][RT][NT];
+    auto& acc = sums[0];
 #pragma unroll
     for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int n = 0; n < NT; ++n) acc[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    lines<XT, FP8, RT, NT, 1, D, kNonTemporal>(acc, wr, woff, rb, xr, xoff, d * (int)sizeof(XT), 0,
-                                               sc, l0, l1, ring);
+    lines<XT, FP8, RT, NT, 1, 1, D>(sums, wr, woff, rb, xr, xoff, d * (int)sizeof(XT), 0, sc, l0,
+                                    l1, ring);
     auto finish = [&](int q, const f32x4_t& sg, const f32x4_t& su) {
         // lane (i, g) holds token i, neurons 4 g ..
         const int nr = q / NT, n = q - nr * NT;
@@ -499,6 +518,22 @@ __device__ __forceinline__ float part_factor<f16_t>(int p) {
     return p == 0 ? kHalfUp : kHalfUp / 2048.0f;
 }
 
+// acc[0] = the sum of the parts' totals
+template <typename HT, int SUMS, int RT, int NT>
+__device__ __forceinline__ void join_parts(f32x4_t (&acc)[SUMS][RT][NT]) {
+    if constexpr (SUMS > 1) {
+        static_assert(SUMS == 2, "hi and lo");
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    acc[0][r][n][e] = fmaf(part_factor<HT>(0), acc[0][r][n][e],
+                                           part_factor<HT>(1) * acc[1][r][n][e]);
+    }
+}
+
 template <typename HT, bool FP8, int PARTS, int RING, int WK, int RT, int NT>
 __device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int d, const uint8_t* dn,
                                           const float* dns, int I, int c0, const uint16_t* list,
@@ -532,41 +567,18 @@ __device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int d, con
         sc[r] = FP8 ? dns + (int64_t)(min(c0 + 16 * r, d - 1) / 128) * nl : nullptr;
     int l0, l1;
     wave_lines<WK>(nl, wk, l0, l1);
-    f32x4_t acc[RT][NT];
+    constexpr int SUMS = std::is_same<HT, f16_t>::value ? PARTS : 1;
+    constexpr int D = ring_depth<RING, FP8, RT, NT, PARTS>();
+    f32x4_t acc[SUMS][RT][NT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int q = 0; q < SUMS; ++q)
 #pragma unroll
-        for (int n = 0; n < NT; ++n) acc[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-    if constexpr (std::is_same<HT, f16_t>::value) {
-        // parts of different weight: one product each
-        constexpr int D = ring_depth<RING, FP8, RT, NT, 1>();
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
-        for (int p = PARTS - 1; p >= 0; --p) {
-            f32x4_t t[RT][NT];
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int n = 0; n < NT; ++n) t[r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
-            int xp[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) xp[n][h] = xoff[n][h] >= 0 ? xoff[n][h] + p * pl : kOOB;
-            lines<HT, FP8, RT, NT, 1, D, 0>(t, wr, woff, rb, hr, xp, hb, 0, sc, l0, l1, ring);
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        acc[r][n][e] = fmaf(part_factor<HT>(p), t[r][n][e], acc[r][n][e]);
-        }
-    } else {
-        constexpr int D = ring_depth<RING, FP8, RT, NT, PARTS>();
-        lines<HT, FP8, RT, NT, PARTS, D, kNonTemporal>(acc, wr, woff, rb, hr, xoff, hb, pl, sc, l0,
-                                                       l1, ring);
-    }
-    join_waves<WK, RT * NT>(&acc[0][0], red, wk, lane, [&](int q, const f32x4_t& s) {
+            for (int n = 0; n < NT; ++n) acc[q][r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    lines<HT, FP8, RT, NT, PARTS, SUMS, D>(acc, wr, woff, rb, hr, xoff, hb, pl, sc, l0, l1, ring);
+    join_parts<HT>(acc);
+    join_waves<WK, RT * NT>(&acc[0][0][0], red, wk, lane, [&](int q, const f32x4_t& s) {
         const int r = q / NT, n = q - r * NT;
         const int c = c0 + 16 * r + 4 * g;
         // d is a multiple of 4: a lane's four columns are all in or all out
@@ -582,7 +594,7 @@ __global__ __launch_bounds__(WK * WR * 64) void moe_down(
     float* __restrict__ z) {
     extern __shared__ uint16_t list[];
     constexpr int W = WK * WR;
-    constexpr int MT = max_tiles<RING, FP8, RT, std::is_same<HT, f16_t>::value ? 1 : PARTS>();
+    constexpr int MT = max_tiles<RING, FP8, RT, PARTS>();
     __shared__ __align__(1024) char rings[W * RING];
     __shared__ int cnt[W];
     int e;
@@ -609,6 +621,248 @@ __global__ __launch_bounds__(WK * WR * 64) void moe_down(
             pass(std::integral_constant<int, MT < 2 ? MT : 2>());
         else
             pass(std::integral_constant<int, MT>());
+    }
+}
+
+// ---- many tokens an expert: waves that share the tokens' operand --------------------------------
+// acc as for lines(), of RT row tiles of each of W waves over all lines of K. A stage holds the rows
+// of every wave and, once, the token operand, of which each wave loads its share; S stages. One
+// barrier a line: past it every wave's loads of the line have landed, and the stage of the line
+// before is free.
+template <bool FP8, int RT, int NT, int PARTS, int W>
+constexpr int wide_stage() {
+    return W * 2 * RT + 2 * NT * PARTS * (FP8 ? 2 : 1);
+}
+template <typename XT, bool FP8, int RT, int NT, int PARTS, int SUMS, int W, int S>
+__device__ __forceinline__ void wide_lines(f32x4_t (&acc)[SUMS][RT][NT], __amdgpu_buffer_rsrc_t wr,
+                                           const int (&woff)[RT][2], int rb,
+                                           __amdgpu_buffer_rsrc_t xr, const uint16_t* list, int m,
+                                           int div, int xb, int plane,
+                                           const float* const (&sc)[RT], int nl, char* lds) {
+    using C = Core<XT, FP8>;
+    constexpr int XC = C::XC, XL = 2 * NT * PARTS * XC / W;  // token loads of a wave
+    constexpr int LPW = 2 * RT + XL, STAGE = wide_stage<FP8, RT, NT, PARTS, W>() * 1024;
+    static_assert(XL * W == 2 * NT * PARTS * XC && (S - 2) * LPW <= 63, "loads");
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int i = lane & 15, g = lane >> 4, lr = lane >> 3;
+    const int lcol = ((lane & 7) ^ lr) * 16;
+    // token load q of the stage: 8 tokens (half h of tile n), part p, 128 bytes c of their columns
+    int xo[XL], xc[XL], xp[XL];
+#pragma unroll
+    for (int u = 0; u < XL; ++u) {
+        const int q = wave * XL + u, h = q & 1, c = (q >> 1) % XC, p = (q >> 1) / XC % PARTS;
+        const int n = (q >> 1) / (XC * PARTS), t = 16 * n + 8 * h + lr;
+        xo[u] = t < m ? (int)list[t] / div * xb + lcol : kOOB;
+        xc[u] = c * kLine;
+        xp[u] = p * plane;
+    }
+    auto load = [&](int l, char* at) {
+        const bool in = (l < nl) & (l * kLine + lcol < rb);
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                load_lds16<kNonTemporal>(wr, at + (wave * 2 * RT + 2 * r + h) * 1024,
+                                         (in & (woff[r][h] >= 0)) ? woff[r][h] + lcol : kOOB,
+                                         l * kLine);
+#pragma unroll
+        for (int u = 0; u < XL; ++u) {
+            const int o = l * XC * kLine + xc[u];
+            load_lds16(xr, at + (W * 2 * RT + wave * XL + u) * 1024,
+                       ((l < nl) & (o + lcol < xb) & (xo[u] >= 0)) ? xo[u] : kOOB, xp[u] + o);
+        }
+    };
+#pragma unroll
+    for (int d = 0; d < S - 1; ++d) load(d, lds + d * STAGE);
+    const uint32_t base = lds_addr(lds) + i * kLine;
+    const uint32_t a0 = base + wave * 2048 * RT + (g ^ (i & 7)) * 16;
+    const uint32_t a1 = base + wave * 2048 * RT + ((4 + g) ^ (i & 7)) * 16;
+    const uint32_t xbase = base + W * 2048 * RT;
+    const uint32_t x0 = xbase + (XC == 1 ? (g ^ (i & 7)) : ((2 * g) ^ (i & 7))) * 16;
+    const uint32_t x1 = xbase + (XC == 1 ? ((4 + g) ^ (i & 7)) : ((2 * g + 1) ^ (i & 7))) * 16;
+    int cur = 0, free = S - 1;
+    for (int l = 0; l < nl; ++l) {
+        wait_vm_lds<(S - 2) * LPW>();
+        wg_barrier();
+        load(l + S - 1, lds + free * STAGE);
+        free = cur;
+        const uint32_t at = cur * STAGE;
+        cur = cur + 1 == S ? 0 : cur + 1;
+        V16 a[RT][2], b[NT * PARTS * XC][2];
+        lds_tiles<RT, 0>(a0 + at, a1 + at, a);
+        lds_tiles<NT * PARTS * XC, 0>(x0 + at, x1 + at, b);
+        line_product<XT, FP8, RT, NT, PARTS, SUMS>(acc, a, b, sc, l);
+    }
+    wait_vm_lds<0>();
+    __syncthreads();  // the stages are free again
+}
+
+constexpr int kWide = 4, kWideStages = 3;  // waves
+
+// token tiles a pass of the down product
+template <bool FP8, int PARTS>
+constexpr int wide_tiles() {
+    return FP8 && PARTS == 3 ? 2 : 4;
+}
+// LDS that the two kernels take beside the pairs' list (1 KB: counts, and what __syncthreads_or
+// keeps there)
+template <bool FP8, int PARTS>
+constexpr size_t wide_lds() {
+    constexpr int g = wide_stage<FP8, 4, 4, 1, kWide>();
+    constexpr int h = wide_stage<FP8, 2, wide_tiles<FP8, PARTS>(), PARTS, kWide>();
+    return (size_t)(kWideStages * (g > h ? g : h) + 1) * 1024;
+}
+
+// Work-group: 128 neurons (32 a wave) of one expert.
+
+template <typename XT, bool FP8, int NT, int S>
+__device__ __forceinline__ void gate_up_wide_pass(
+    const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
+    const uint16_t* list, int m, typename HType<XT, FP8>::type* H, int64_t plane, int parts,
+    char* lds) {
+    constexpr int RT = 4;
+    const int lane = threadIdx.x & 63;
+    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
+    const int rb = d * (FP8 ? 1 : (int)sizeof(XT));
+    int woff[RT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int j = n0 + 16 * (r >> 1) + 8 * h + lr;
+            woff[r][h] = j < I ? ((r & 1) * I + j) * rb : kOOB;
+        }
+    const int nl = (rb + kLine - 1) / kLine, nb = (I + 127) / 128;
+    const float* sc[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+        sc[r] = FP8 ? gus + (int64_t)((r & 1) * nb + min(n0 + 16 * (r >> 1), I - 1) / 128) * nl
+                    : nullptr;
+    f32x4_t acc[1][RT][NT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) acc[0][r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    wide_lines<XT, FP8, RT, NT, 1, 1, kWide, S>(
+        acc, make_rsrc(gu, (int64_t)2 * I * rb), woff, rb, make_rsrc(x, xbytes), list, m, k,
+        d * (int)sizeof(XT), 0, sc, nl, lds);
+#pragma unroll
+    for (int q = 0; q < 2 * NT; ++q) {
+        const int nr = q / NT, n = q - nr * NT;
+        if (16 * n + row < m) {
+            const int64_t pair = list[16 * n + row];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = n0 + 16 * nr + 4 * g + e;
+                if (j < I)
+                    put_h(silu_f32(acc[0][2 * nr][n][e]) * acc[0][2 * nr + 1][n][e], pair * I + j,
+                          plane, parts, H);
+            }
+        }
+    }
+}
+
+template <typename XT, bool FP8>
+__global__ __launch_bounds__(kWide * 64) void moe_gate_up_wide(
+    const XT* __restrict__ x, int64_t T, int d, const int32_t* __restrict__ ids, int npairs, int k,
+    const uint8_t* __restrict__ gate_up, const float* __restrict__ scales, int E, int I,
+    int by_pair, typename HType<XT, FP8>::type* __restrict__ H, int parts) {
+    extern __shared__ uint16_t list[];
+    constexpr int S = kWideStages;
+    __shared__ __align__(1024) char lds[S * wide_stage<FP8, 4, 4, 1, kWide>() * 1024];
+    __shared__ int cnt[kWide];
+    int e;
+    const int m = expert_pairs<kWide>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
+    if (m == 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
+    const uint8_t* gu = gate_up + (int64_t)e * 2 * I * d * WB;
+    const int nb = (I + 127) / 128;
+    const float* gs = FP8 ? scales + (int64_t)e * 2 * nb * ((d + 127) / 128) : nullptr;
+    const int n0 = (blockIdx.x * kWide + wave) * 32;
+    const int64_t plane = (int64_t)npairs * I, xb = T * d * (int64_t)sizeof(XT);
+    for (int c = 0; c < m; c += 64) {
+        const int mc = min(m - c, 64);
+        if (mc <= 32)
+            gate_up_wide_pass<XT, FP8, 2, S>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane,
+                                             parts, lds);
+        else
+            gate_up_wide_pass<XT, FP8, 4, S>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane,
+                                             parts, lds);
+    }
+}
+
+// Work-group: 128 rows (32 a wave) of one expert's down matrix.
+template <typename HT, bool FP8, int PARTS, int NT, int S>
+__device__ __forceinline__ void down_wide_pass(const HT* H, int64_t plane, int d, const uint8_t* dn,
+                                               const float* dns, int I, int c0,
+                                               const uint16_t* list, int m, float* z, char* lds) {
+    constexpr int RT = 2, SUMS = std::is_same<HT, f16_t>::value ? PARTS : 1;
+    const int lane = threadIdx.x & 63;
+    const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
+    const int rb = I * (FP8 ? 1 : (int)sizeof(HT));
+    int woff[RT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            const int c = c0 + 16 * r + 8 * h + lr;
+            woff[r][h] = c < d ? c * rb : kOOB;
+        }
+    const int nl = (rb + kLine - 1) / kLine;
+    const float* sc[RT];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+        sc[r] = FP8 ? dns + (int64_t)(min(c0 + 16 * r, d - 1) / 128) * nl : nullptr;
+    f32x4_t acc[SUMS][RT][NT];
+#pragma unroll
+    for (int q = 0; q < SUMS; ++q)
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int n = 0; n < NT; ++n) acc[q][r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    wide_lines<HT, FP8, RT, NT, PARTS, SUMS, kWide, S>(
+        acc, make_rsrc(dn, (int64_t)d * rb), woff, rb,
+        make_rsrc(H, (int64_t)PARTS * plane * sizeof(HT)), list, m, 1, I * (int)sizeof(HT),
+        (int)(plane * sizeof(HT)), sc, nl, lds);
+    join_parts<HT>(acc);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const int c = c0 + 16 * r + 4 * g;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            // d is a multiple of 4: a lane's four columns are all in or all out
+            if (16 * n + row < m && c < d)
+                *reinterpret_cast<f32x4_t*>(z + (int64_t)list[16 * n + row] * d + c) = acc[0][r][n];
+        }
+    }
+}
+
+template <typename HT, bool FP8, int PARTS>
+__global__ __launch_bounds__(kWide * 64) void moe_down_wide(
+    const HT* __restrict__ H, int d, const int32_t* __restrict__ ids, int npairs,
+    const uint8_t* __restrict__ down, const float* __restrict__ scales, int E, int I, int by_pair,
+    float* __restrict__ z) {
+    extern __shared__ uint16_t list[];
+    constexpr int NTM = wide_tiles<FP8, PARTS>(), S = kWideStages;
+    __shared__ __align__(1024) char lds[S * wide_stage<FP8, 2, NTM, PARTS, kWide>() * 1024];
+    __shared__ int cnt[kWide];
+    int e;
+    const int m = expert_pairs<kWide>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
+    if (m == 0) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const uint8_t* dn = down + (int64_t)e * d * I * (FP8 ? 1 : (int)sizeof(HT));
+    const float* ds = FP8 ? scales + (int64_t)e * ((d + 127) / 128) * ((I + 127) / 128) : nullptr;
+    const int c0 = (blockIdx.x * kWide + wave) * 32;
+    const int64_t plane = (int64_t)npairs * I;
+    for (int c = 0; c < m; c += 16 * NTM) {
+        const int mc = min(m - c, 16 * NTM);
+        if (mc <= 32)
+            down_wide_pass<HT, FP8, PARTS, 2, S>(H, plane, d, dn, ds, I, c0, list + c, mc, z, lds);
+        else
+            down_wide_pass<HT, FP8, PARTS, NTM, S>(H, plane, d, dn, ds, I, c0, list + c, mc, z,
+                                                   lds);
     }
 }
 
@@ -959,12 +1213,13 @@ void sum(const Args& a, YT* y) {
 // with rows of 1408, 11 lines: down by 1 wave 159, by 2 187).
 constexpr int kLongRow = 64;
 
-// Pairs an expert from which the tokens' operand, which every wave loads for its own rows, weighs
-// more than the weights: tiles of twice the rows for 64 tokens (8 experts of 4096 x 4096, bf16, 24
-// pairs an expert 197 us by the small tiles and 203 by the large, 64 pairs 445 and 312; 8-bit
-// experts 163 and 145, 342 and 265; 16 pairs an expert, 128 experts of 768 x 2048: 327 and 355).
-// float32 products are bound by their MFMAs, where the large tiles are no help (398 and 723 us).
-constexpr int64_t kManyPairs = 28;
+// Pairs an expert from which the tokens' operand weighs: waves that share it, instead of each
+// loading it for its own rows. Microseconds by the kernels of few and of many tokens:
+//   8 experts of 14336 x 4096, bf16: 12 pairs each 473 and 504, 16: 515 and 508, 32: 831 and 550,
+//     100: 2176 and 1126;  128 of 768 x 2048, bf16: 8: 256 and 270, 12: 284 and 280, 25: 440, 325
+//   64 of 1408 x 4096, 8-bit: 9: 252 and 275, 12: 276 and 280, 18: 365 and 297, 37: 708 and 381
+// float32 products are bound by their MFMAs, where sharing is no help.
+constexpr int64_t kManyPairs = 14;
 
 template <typename XT, bool FP8, int PARTS>
 void experts(const Args& a) {
@@ -980,7 +1235,9 @@ void experts(const Args& a) {
     const int gl = (int)((a.d * (FP8 ? 1 : (int)sizeof(XT)) + kLine - 1) / kLine);
     const int dl = (int)((a.I * (FP8 ? 1 : (int)sizeof(HT)) + kLine - 1) / kLine);
     constexpr bool kMany = sizeof(XT) == 2;
-    const bool many = kMany && (int64_t)np >= kManyPairs * a.E;
+    // (lists of more than 7680 pairs do not fit beside the stages of 8-bit weights)
+    const bool many =
+        kMany && (int64_t)np >= kManyPairs * a.E && wide_lds<FP8, PARTS>() + lds <= 160 * 1024;
     const XT* x = static_cast<const XT*>(a.x);
     const int64_t xlds = one_pitch(a.d, sizeof(XT));
     if (a.T == 1 && xlds <= kOneX) {
@@ -1000,7 +1257,7 @@ void experts(const Args& a) {
                 by_pair, H, a.p.parts);
         };
         if (many) {
-            if constexpr (kMany) gate(moe_gate_up<XT, FP8, 48 * 1024, 2, 2>, 32, 128);
+            if constexpr (kMany) gate(moe_gate_up_wide<XT, FP8>, 32 * kWide, kWide * 64);
         } else if (gl >= kLongRow) {
             gate(moe_gate_up<XT, FP8, 16 * 1024, 4, 1>, 16, 256);
         } else {
@@ -1033,7 +1290,7 @@ void experts(const Args& a) {
             H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
     };
     if (many) {
-        if constexpr (kMany) down(moe_down<HT, FP8, PARTS, 48 * 1024, 1, 2, 4>, 128, 128);
+        if constexpr (kMany) down(moe_down_wide<HT, FP8, PARTS>, 32 * kWide, kWide * 64);
     } else if (dl >= kLongRow) {
         down(moe_down<HT, FP8, PARTS, 24 * 1024, 2, 2, 2>, 64, 256);
     } else {

@@ -177,6 +177,10 @@ LAYERS = [
     (1, 300, 3, 64, 48), (1, 200, 6, 64, 2064), (1, 16, 10, 4368, 32), (1, 256, 32, 256, 16),
     # long rows; the most tokens and pairs
     (3, 4, 2, 8208, 16), (3, 4, 2, 48, 8208), (512, 20, 16, 64, 32),
+    (480, 16, 16, 64, 32),
+    # many tokens an expert, over several lines of both products: one, two and more passes, the
+    # last of up to 32 tokens and of more
+    (90, 2, 2, 400, 272), (200, 3, 1, 1040, 528), (100, 3, 1, 144, 1552), (170, 2, 1, 784, 144),
 ]
 
 
