@@ -700,18 +700,33 @@ __device__ __forceinline__ void wide_lines(f32x4_t (&acc)[SUMS][RT][NT], __amdgp
 
 constexpr int kWide = 4, kWideStages = 3;  // waves
 
-// token tiles a pass of the down product
+// most token tiles a pass, by the LDS that three stages of them take
 template <bool FP8, int PARTS>
 constexpr int wide_tiles() {
-    return FP8 && PARTS == 3 ? 2 : 4;
+    return FP8 ? (PARTS == 3 ? 2 : 4) : (PARTS == 3 ? 4 : 8);
 }
 // LDS that the two kernels take beside the pairs' list (1 KB: counts, and what __syncthreads_or
 // keeps there)
 template <bool FP8, int PARTS>
 constexpr size_t wide_lds() {
-    constexpr int g = wide_stage<FP8, 4, 4, 1, kWide>();
+    constexpr int g = wide_stage<FP8, 4, wide_tiles<FP8, 1>(), 1, kWide>();
     constexpr int h = wide_stage<FP8, 2, wide_tiles<FP8, PARTS>(), PARTS, kWide>();
     return (size_t)(kWideStages * (g > h ? g : h) + 1) * 1024;
+}
+
+// m pairs in passes of up to NTM tiles, the fewest tiles of 2, 4 and 8 that hold a pass:
+// pass(tiles, first pair, pairs)
+template <int NTM, typename F>
+__device__ __forceinline__ void wide_passes(int m, F pass) {
+    for (int c = 0; c < m; c += 16 * NTM) {
+        const int mc = min(m - c, 16 * NTM);
+        if (NTM == 2 || mc <= 32)
+            pass(std::integral_constant<int, 2>(), c, mc);
+        else if (NTM == 4 || mc <= 64)
+            pass(std::integral_constant<int, NTM < 4 ? NTM : 4>(), c, mc);
+        else
+            pass(std::integral_constant<int, NTM>(), c, mc);
+    }
 }
 
 // Work-group: 128 neurons (32 a wave) of one expert.
@@ -769,8 +784,8 @@ __global__ __launch_bounds__(kWide * 64) void moe_gate_up_wide(
     const uint8_t* __restrict__ gate_up, const float* __restrict__ scales, int E, int I,
     int by_pair, typename HType<XT, FP8>::type* __restrict__ H, int parts) {
     extern __shared__ uint16_t list[];
-    constexpr int S = kWideStages;
-    __shared__ __align__(1024) char lds[S * wide_stage<FP8, 4, 4, 1, kWide>() * 1024];
+    constexpr int NTM = wide_tiles<FP8, 1>(), S = kWideStages;
+    __shared__ __align__(1024) char lds[S * wide_stage<FP8, 4, NTM, 1, kWide>() * 1024];
     __shared__ int cnt[kWide];
     int e;
     const int m = expert_pairs<kWide>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
@@ -782,15 +797,10 @@ __global__ __launch_bounds__(kWide * 64) void moe_gate_up_wide(
     const float* gs = FP8 ? scales + (int64_t)e * 2 * nb * ((d + 127) / 128) : nullptr;
     const int n0 = (blockIdx.x * kWide + wave) * 32;
     const int64_t plane = (int64_t)npairs * I, xb = T * d * (int64_t)sizeof(XT);
-    for (int c = 0; c < m; c += 64) {
-        const int mc = min(m - c, 64);
-        if (mc <= 32)
-            gate_up_wide_pass<XT, FP8, 2, S>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane,
-                                             parts, lds);
-        else
-            gate_up_wide_pass<XT, FP8, 4, S>(x, xb, d, k, gu, gs, I, n0, list + c, mc, H, plane,
-                                             parts, lds);
-    }
+    wide_passes<NTM>(m, [&](auto tiles, int c, int mc) {
+        gate_up_wide_pass<XT, FP8, decltype(tiles)::value, S>(x, xb, d, k, gu, gs, I, n0, list + c,
+                                                              mc, H, plane, parts, lds);
+    });
 }
 
 // Work-group: 128 rows (32 a wave) of one expert's down matrix.
@@ -856,14 +866,10 @@ __global__ __launch_bounds__(kWide * 64) void moe_down_wide(
     const float* ds = FP8 ? scales + (int64_t)e * ((d + 127) / 128) * ((I + 127) / 128) : nullptr;
     const int c0 = (blockIdx.x * kWide + wave) * 32;
     const int64_t plane = (int64_t)npairs * I;
-    for (int c = 0; c < m; c += 16 * NTM) {
-        const int mc = min(m - c, 16 * NTM);
-        if (mc <= 32)
-            down_wide_pass<HT, FP8, PARTS, 2, S>(H, plane, d, dn, ds, I, c0, list + c, mc, z, lds);
-        else
-            down_wide_pass<HT, FP8, PARTS, NTM, S>(H, plane, d, dn, ds, I, c0, list + c, mc, z,
-                                                   lds);
-    }
+    wide_passes<NTM>(m, [&](auto tiles, int c, int mc) {
+        down_wide_pass<HT, FP8, PARTS, decltype(tiles)::value, S>(H, plane, d, dn, ds, I, c0,
+                                                                  list + c, mc, z, lds);
+    });
 }
 
 // ---- weighted sum ----------------------------------------------------------------------------
