@@ -431,7 +431,8 @@ int si_load_selected(const void* w_gate, const void* w_up, const void* w_down, i
  *
  * in float32, codes rounded to nearest even. A block that holds a NaN or an infinity gets scale
  * NaN and NaN codes. Requires G, R >= 0, C >= 1, C % 16 == 0, 16-byte aligned x and codes, fewer
- * than 2^28 (block_rows = 1) or 2^23 blocks. G * R = 0 enqueues nothing. Asynchronous, stream-ordered.
+ * than 2^28 (block_rows = 1) or 2^23 blocks. G * R = 0 enqueues nothing. Asynchronous,
+ * stream-ordered.
  */
 int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C, int block_rows,
                     uint8_t* codes, float* scales, void* hip_stream);
@@ -522,13 +523,12 @@ int si_moe_route(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* 
  * Accumulation is float32; h = SiLU(g) * u is float32 and enters the down product as float32
  * (float32 weights), as bf16 parts of 16 significant bits in all (24 with a float32 y), or with
  * half weights as a half pair of 22 bits for |h| < 2^24. Each chosen expert's weights are read
- * once per 16 to 64 of its tokens. An infinite down weight of 16 bits may give NaN where the
+ * once per 16 to 128 of its tokens. An infinite down weight of 16 bits may give NaN where the
  * formula gives an infinity (it meets the lower parts of h). Requires 0 <= T <= 512,
  * 1 <= k <= 32, T * k <= 8192, 1 <= E <= 65535; d and I multiples of 4 (float32), 8 (16-bit) or
  * 16 (SI_E4M3), d, I <= 65536; one expert's gate and up rows, x as float32, and the parts of h
  * (T * k * I values) each below 2 GiB, else SI_ERR_UNSUPPORTED; 16-byte aligned x, gate_up, down,
- * y and ws. Asynchronous, stream-ordered,
- * deterministic.
+ * y and ws. Asynchronous, stream-ordered, deterministic.
  */
 size_t si_moe_ffn_workspace(int64_t T, int64_t k, int64_t E, int64_t d, int64_t I, si_dtype xdt,
                             si_dtype wdt, si_dtype ydt);

@@ -3,7 +3,7 @@
 //   y[t] = sum over r < k of w[t][r] * D_e (SiLU(G_e x[t]) * (U_e x[t])),   e = ids[t][r]
 //
 // gate_up [E][2][I][d] and down [E][d][I] are read where they lie, each chosen expert once per 16
-// to 64 of its tokens: with few tokens the time is that of streaming the chosen experts' weights,
+// to 128 of its tokens: with few tokens the time is that of streaming the chosen experts' weights,
 // and every product runs on MFMAs whose token operand is mostly padding (16 tokens a tile), which
 // is free below the weights' rate. Three kernels: gate/up with SiLU(g) * u, down, weighted sum; two
 // for one token, the router's choice included; two others for many tokens an expert, whose waves
@@ -625,8 +625,8 @@ __global__ __launch_bounds__(WK * WR * 64) void moe_down(
 }
 
 // ---- many tokens an expert: waves that share the tokens' operand --------------------------------
-// acc as for lines(), of RT row tiles of each of W waves over all lines of K. A stage holds the rows
-// of every wave and, once, the token operand, of which each wave loads its share; S stages. One
+// acc as for lines(), of RT row tiles of each of W waves over all lines of K. A stage holds every
+// wave's rows and, once, the token operand, of which each wave loads its share; S stages. One
 // barrier a line: past it every wave's loads of the line have landed, and the stage of the line
 // before is free.
 template <bool FP8, int RT, int NT, int PARTS, int W>
@@ -1221,10 +1221,13 @@ constexpr int kLongRow = 64;
 
 // Pairs an expert from which the tokens' operand weighs: waves that share it, instead of each
 // loading it for its own rows. Microseconds by the kernels of few and of many tokens:
-//   8 experts of 14336 x 4096, bf16: 12 pairs each 473 and 504, 16: 515 and 508, 32: 831 and 550,
-//     100: 2176 and 1126;  128 of 768 x 2048, bf16: 8: 256 and 270, 12: 284 and 280, 25: 440, 325
-//   64 of 1408 x 4096, 8-bit: 9: 252 and 275, 12: 276 and 280, 18: 365 and 297, 37: 708 and 381
-// float32 products are bound by their MFMAs, where sharing is no help.
+//   8 experts of 14336 x 4096, bf16: 12 pairs each 474 and 503, 16: 512 and 508, 32: 862 and 553,
+//     100: 2170 and 756;  128 of 768 x 2048, bf16: 8: 253 and 271, 12: 284 and 284, 25: 437, 325
+//   64 of 1408 x 4096, 8-bit: 9: 253 and 270, 12: 280 and 275, 18: 356 and 294, 37: 703 and 379
+//   half, 8 of 8192 x 4096: 16: 296 and 354, 32: 495 and 352;  64 of 1024 x 1024: 6: 97 and 84,
+//     16: 126 and 93
+// (Up to six stages where passes are narrow: no change.) float32 products are bound by their MFMAs,
+// where sharing is no help.
 constexpr int64_t kManyPairs = 14;
 
 template <typename XT, bool FP8, int PARTS>
