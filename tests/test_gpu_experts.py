@@ -7,6 +7,8 @@ Layer: the oracle carries the bound of float32 arithmetic through (oracle.moe_ff
 down product with 2^-16 of its value (bf16 pair), 2^-24 (three bf16 parts, float32) or 2^-22 and
 2^-28 absolutely (half pair), and the output half a step of its type.
 """
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -239,10 +241,11 @@ def test_caller_ids(T, dt, wkind):
         else None
 
 
-def test_values_stay_in_their_token():
+@pytest.mark.parametrize("T", [20, 150])
+def test_values_stay_in_their_token(T):
     """NaN and infinities of a token, or of an expert, reach only the tokens that use them."""
-    say("layer: NaN and infinities")
-    E, d, inter, T, k = 4, 64, 48, 20, 1
+    say(f"layer: NaN and infinities T={T}")
+    E, d, inter, k = 4, 64, 48, 1
     dev, gu, dn = _experts(E, d, inter, "bf16", "same", 1)
     x = torch.randn(T, d, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
     ids = (torch.arange(T, dtype=torch.int32, device=DEV) % E).view(T, 1)
@@ -259,7 +262,7 @@ def test_values_stay_in_their_token():
     assert not torch.any(torch.isfinite(y[8]))
 
 
-@pytest.mark.parametrize("T", [1, 5])
+@pytest.mark.parametrize("T", [1, 5, 70])
 def test_nan_codes(T):
     """A NaN code, or a NaN scale, of an 8-bit expert reaches the tokens that use it and no other."""
     say(f"layer: NaN codes T={T}")
@@ -275,11 +278,11 @@ def test_nan_codes(T):
     assert torch.all(torch.isnan(run(1))) and torch.all(torch.isnan(run(2)))
 
 
-@pytest.mark.parametrize("dt", ["f16", "bf16"])
-def test_large_and_small_h(dt):
+@pytest.mark.parametrize("dt,T", [("f16", 9), ("bf16", 9), ("f16", 75), ("bf16", 75)])
+def test_large_and_small_h(dt, T):
     """h from 2^-20 to 2^20: beyond what one half value holds at either end."""
-    say(f"layer: large and small h {dt}")
-    E, d, inter, T = 1, 64, 64, 9
+    say(f"layer: large and small h {dt} T={T}")
+    E, d, inter = 1, 64, 64
     g = torch.Generator().manual_seed(2)
     gu = torch.randn(E, 2, inter, d, generator=g).to(DT[dt])
     dn = (torch.randn(E, d, inter, generator=g) / 8).to(DT[dt])
@@ -288,8 +291,13 @@ def test_large_and_small_h(dt):
     ids = torch.zeros(T, 1, dtype=torch.int32)
     weights = torch.ones(T, 1)
     y = si.moe_ffn(x.to(DEV), ids.to(DEV), weights.to(DEV), gu.to(DEV), dn.to(DEV))
-    assert torch.all(torch.isfinite(y))
-    _check_layer(y, x, ids, weights, gu.double().numpy(), dn.double().numpy(), dt, "same")
+    # half weights promise |h| < 2^24 (one token of the 75 lies past it, at 2^24.2)
+    G, U = (x.double() @ gu[0, i].double().t() for i in (0, 1))
+    ok = (G / (1 + torch.exp(-G)) * U).abs().amax(dim=1) < (2.0 ** 24 if dt == "f16" else math.inf)
+    assert int((~ok).sum()) == (1 if (dt, T) == ("f16", 75) else 0)
+    assert torch.all(torch.isfinite(y[ok.to(DEV)]))
+    _check_layer(y[ok.to(DEV)], x[ok], ids[ok], weights[ok], gu.double().numpy(),
+                 dn.double().numpy(), dt, "same")
 
 
 @pytest.mark.parametrize("T,dt,wkind", [(1, "bf16", "same"), (6, "bf16", "fp8"), (90, "f16", "same")])
