@@ -729,14 +729,15 @@ __device__ __forceinline__ void wide_passes(int m, F pass) {
     }
 }
 
-// Work-group: 128 neurons (32 a wave) of one expert.
+// Work-group: 64 NR neurons (16 NR a wave) of one expert. NR = 1 takes passes of up to 64 tokens in
+// 72 KB of LDS, so that two work-groups share a CU; NR = 2 of up to 128 (8-bit weights 64).
 
-template <typename XT, bool FP8, int NT, int S>
+template <typename XT, bool FP8, int NR, int NT, int S>
 __device__ __forceinline__ void gate_up_wide_pass(
     const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
     const uint16_t* list, int m, typename HType<XT, FP8>::type* H, int64_t plane, int parts,
     char* lds) {
-    constexpr int RT = 4;
+    constexpr int RT = 2 * NR;
     const int lane = threadIdx.x & 63;
     const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
     const int rb = d * (FP8 ? 1 : (int)sizeof(XT));
@@ -763,7 +764,7 @@ __device__ __forceinline__ void gate_up_wide_pass(
         acc, make_rsrc(gu, (int64_t)2 * I * rb), woff, rb, make_rsrc(x, xbytes), list, m, k,
         d * (int)sizeof(XT), 0, sc, nl, lds);
 #pragma unroll
-    for (int q = 0; q < 2 * NT; ++q) {
+    for (int q = 0; q < NR * NT; ++q) {
         const int nr = q / NT, n = q - nr * NT;
         if (16 * n + row < m) {
             const int64_t pair = list[16 * n + row];
@@ -778,14 +779,14 @@ __device__ __forceinline__ void gate_up_wide_pass(
     }
 }
 
-template <typename XT, bool FP8>
+template <typename XT, bool FP8, int NR>
 __global__ __launch_bounds__(kWide * 64) void moe_gate_up_wide(
     const XT* __restrict__ x, int64_t T, int d, const int32_t* __restrict__ ids, int npairs, int k,
     const uint8_t* __restrict__ gate_up, const float* __restrict__ scales, int E, int I,
     int by_pair, typename HType<XT, FP8>::type* __restrict__ H, int parts) {
     extern __shared__ uint16_t list[];
-    constexpr int NTM = wide_tiles<FP8, 1>(), S = kWideStages;
-    __shared__ __align__(1024) char lds[S * wide_stage<FP8, 4, NTM, 1, kWide>() * 1024];
+    constexpr int NTM = NR == 1 ? 4 : wide_tiles<FP8, 1>(), S = kWideStages;
+    __shared__ __align__(1024) char lds[S * wide_stage<FP8, 2 * NR, NTM, 1, kWide>() * 1024];
     __shared__ int cnt[kWide];
     int e;
     const int m = expert_pairs<kWide>(ids, npairs, E, blockIdx.y, by_pair, e, list, cnt);
@@ -795,11 +796,12 @@ __global__ __launch_bounds__(kWide * 64) void moe_gate_up_wide(
     const uint8_t* gu = gate_up + (int64_t)e * 2 * I * d * WB;
     const int nb = (I + 127) / 128;
     const float* gs = FP8 ? scales + (int64_t)e * 2 * nb * ((d + 127) / 128) : nullptr;
-    const int n0 = (blockIdx.x * kWide + wave) * 32;
+    const int n0 = (blockIdx.x * kWide + wave) * 16 * NR;
     const int64_t plane = (int64_t)npairs * I, xb = T * d * (int64_t)sizeof(XT);
     wide_passes<NTM>(m, [&](auto tiles, int c, int mc) {
-        gate_up_wide_pass<XT, FP8, decltype(tiles)::value, S>(x, xb, d, k, gu, gs, I, n0, list + c,
-                                                              mc, H, plane, parts, lds);
+        gate_up_wide_pass<XT, FP8, NR, decltype(tiles)::value, S>(x, xb, d, k, gu, gs, I, n0,
+                                                                  list + c, mc, H, plane, parts,
+                                                                  lds);
     });
 }
 
@@ -1221,14 +1223,19 @@ constexpr int kLongRow = 64;
 
 // Pairs an expert from which the tokens' operand weighs: waves that share it, instead of each
 // loading it for its own rows. Microseconds by the kernels of few and of many tokens:
-//   8 experts of 14336 x 4096, bf16: 12 pairs each 474 and 503, 16: 512 and 508, 32: 862 and 553,
-//     100: 2170 and 756;  128 of 768 x 2048, bf16: 8: 253 and 271, 12: 284 and 284, 25: 437, 325
+//   8 experts of 14336 x 4096, bf16: 12 pairs each 472 and 494, 16: 512 and 496, 32: 862 and 530;
+//   128 of 768 x 2048, bf16: 8: 253 and 251, 12: 284 and 262, 16: 315 and 272
 //   64 of 1408 x 4096, 8-bit: 9: 253 and 270, 12: 280 and 275, 18: 356 and 294, 37: 703 and 379
-//   half, 8 of 8192 x 4096: 16: 296 and 354, 32: 495 and 352;  64 of 1024 x 1024: 6: 97 and 84,
-//     16: 126 and 93
-// (Up to six stages where passes are narrow: no change.) float32 products are bound by their MFMAs,
-// where sharing is no help.
-constexpr int64_t kManyPairs = 14;
+//   half, 8 of 8192 x 4096: 12: 279 and 314, 16: 296 and 318, 32: 495 and 326;  64 of 1024 x 1024:
+//     12: 114 and 87
+// float32 products are bound by their MFMAs, where sharing is no help.
+constexpr int64_t kManyPairs = 16;
+
+// Pairs an expert up to which gate and up take two work-groups a CU and passes of 64 tokens: 8
+// experts of 14336 x 4096, 24 pairs 483 us, by wider ones 522; 48: 549 and 571; 64, where half of
+// the experts take two passes: 819 and 682. (8-bit weights: no difference. Down with two
+// work-groups a CU, by half the rows or two stages: from 6% less to 18% more.)
+constexpr int64_t kWidePairs = 48;
 
 template <typename XT, bool FP8, int PARTS>
 void experts(const Args& a) {
@@ -1266,7 +1273,14 @@ void experts(const Args& a) {
                 by_pair, H, a.p.parts);
         };
         if (many) {
-            if constexpr (kMany) gate(moe_gate_up_wide<XT, FP8>, 32 * kWide, kWide * 64);
+            if constexpr (FP8) {
+                gate(moe_gate_up_wide<XT, true, 2>, 32 * kWide, kWide * 64);
+            } else if constexpr (kMany) {
+                if (np <= kWidePairs * a.E)
+                    gate(moe_gate_up_wide<XT, false, 1>, 16 * kWide, kWide * 64);
+                else
+                    gate(moe_gate_up_wide<XT, false, 2>, 32 * kWide, kWide * 64);
+            }
         } else if (gl >= kLongRow) {
             gate(moe_gate_up<XT, FP8, 16 * 1024, 4, 1>, 16, 256);
         } else {

@@ -183,6 +183,7 @@ LAYERS = [
     # many tokens an expert, over several lines of both products: one, two and more passes, the
     # last of up to 32 tokens and of more
     (90, 2, 2, 400, 272), (200, 3, 1, 1040, 528), (100, 3, 1, 144, 1552), (170, 2, 1, 784, 144),
+    (45, 3, 1, 656, 400), (33, 4, 2, 272, 80),
 ]
 
 
