@@ -16,7 +16,7 @@
 //
 // Rates (weights of the experts that were chosen): 48 tokens over 8 experts of 14336 x 4096 in bf16
 // 486 us, 5.8 TB/s; 13 tokens over 64 8-bit experts of 1408 x 4096 157 us, 5.1 TB/s; one token
-// through 8 of 128 experts of 768 x 2048 25.6 us, of which three launches cost about 7.
+// through 8 of 128 experts of 768 x 2048 24.5 us, of which three launches cost about 7.
 //
 // Element types: float32, bf16, half, or e4m3 codes with a float32 scale for each 128 x 128
 // weights. Codes become the 16-bit type of x (exactly); a scale block's products are summed in

@@ -110,9 +110,19 @@ __device__ __forceinline__ void choose_experts(const Choice& a, int t, bool publ
         const int parts = (int)blockDim.x / a.EP, per = (E + parts - 1) / parts;
         const int lo = min(E, (i / a.EP) * per), hi = min(E, lo + per);
         const uint64_t m = s.keys[me];
+        // (an equal key goes first from a lower expert; which side of a lane's own an expert lies on
+        // is open only among the wave's own 64: 200 tokens, 256 experts 20.9 -> 19.0 us)
+        const int own = __builtin_amdgcn_readfirstlane(me & ~63);
         int n = 0;
+        auto count = [&](int from, int to, uint64_t past) {
 #pragma unroll 8
-        for (int j = lo; j < hi; ++j) n += s.keys[j] > m - (uint64_t)(j < me);
+            for (int j = from; j < to; ++j) n += s.keys[j] > past;
+        };
+        count(lo, min(hi, own), m - 1u);
+#pragma unroll 8
+        for (int j = max(lo, own); j < min(hi, own + 64); ++j)
+            n += s.keys[j] > m - (uint64_t)(j < me);
+        count(max(lo, own + 64), hi, m);
         if (n) atomicAdd(&s.rank[me], n);  // whole numbers: the order of the additions is free
     }
     __syncthreads();
