@@ -110,7 +110,7 @@ __device__ __forceinline__ void choose_experts(const Choice& a, int t, bool publ
         const int parts = (int)blockDim.x / a.EP, per = (E + parts - 1) / parts;
         const int lo = min(E, (i / a.EP) * per), hi = min(E, lo + per);
         const uint64_t m = s.keys[me];
-        // (an equal key goes first from a lower expert; which side of a lane's own an expert lies on
+        // (an equal key goes first from a lower expert; on which side of a lane's own an expert is,
         // is open only among the wave's own 64: 200 tokens, 256 experts 20.9 -> 19.0 us)
         const int own = __builtin_amdgcn_readfirstlane(me & ~63);
         int n = 0;
