@@ -70,22 +70,17 @@ __device__ __forceinline__ void put(bf16_t* y, float v) {
     *y = __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 __device__ __forceinline__ void put(f16_t* y, float v) { *y = (f16_t)v; }
-// eight values at an 8-element aligned place
-__device__ __forceinline__ void put8(float* y, const f32x4_t& a, const f32x4_t& b) {
-    *reinterpret_cast<f32x4_t*>(y) = a;
-    *reinterpret_cast<f32x4_t*>(y + 4) = b;
-}
-template <typename T16>
-__device__ __forceinline__ void put8(T16* y, const f32x4_t& a, const f32x4_t& b) {
-    T16 o[8];
+// eight values at any place (rows of y whose length is no multiple of 8; one vector store for 16
+// bytes all the same: by single values 2079 tokens, 14146 x 8176, took 337 us instead of 297)
+template <typename YT>
+__device__ __forceinline__ void put8(YT* y, const f32x4_t& a, const f32x4_t& b) {
+    YT o[8];
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         put(o + e, a[e]);
         put(o + 4 + e, b[e]);
     }
-    V16 u;
-    __builtin_memcpy(&u, o, 16);
-    st16(y, u);
+    __builtin_memcpy(y, o, sizeof(o));
 }
 // four values at a 4-element aligned place
 __device__ __forceinline__ void put4(float* y, const f32x4_t& v) {
@@ -260,7 +255,10 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
     // The tiles that an XCD works on at a time read the same rows in step, so that each step's
     // lines would be first read, by all of them, one step before their use. Each of them also
     // touches its share of the lines of a later step (one word a line, into LDS that nothing
-    // reads), which then come from the XCD's L2.
+    // reads), which then come from the XCD's L2. The word is the block's last: where K is no
+    // multiple of 128, blocks begin and end inside lines, and the first line was touched a step
+    // before (4096 tokens, 14336 x 4112: 326 us by the blocks' first words, 287 by the last; 2079,
+    // 14146 x 8176: 295 and 307; K = 4096: 247 and 248).
     const int sharew = min(8, ntm), sharex = max(1, 32 / sharew);
     const int rx = (BM + sharex - 1) / sharex, rw = (BN + sharew - 1) / sharew;
     constexpr int kLoads = LA + LB + (TOUCH ? 2 : 1);
@@ -297,8 +295,9 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
         __builtin_amdgcn_raw_ptr_buffer_load_lds(ls, (lds_void*)(at + kScale + sg * 256), 4,
                                                  lb < lb1 ? vs : kOOB, lb * 4, 0, 0);
         if (TOUCH)
-            __builtin_amdgcn_global_load_lds((global_void*)(pf + min(lb + 1, lb1 - 1) * kBlk),
-                                             (lds_void*)(touched + wave * 256), 4, 0, 0);
+            __builtin_amdgcn_global_load_lds(
+                (global_void*)(pf + min(min(lb + 2, lb1) * kBlk, K) - 4),
+                (lds_void*)(touched + wave * 256), 4, 0, 0);
         ++lb;
     };
     f32x4_t acc[RN][RM];
@@ -410,8 +409,8 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
 #pragma unroll
             for (int n = 0; n < RN; n += 2) {
                 const int c = it.tn * BN + wn * TN + 16 * n + 8 * g;
-                if ((N & 7) == 0) {
-                    if (c < N) put8(out + (int64_t)tk * N + c, acc[n][m], acc[n + 1][m]);
+                if (c + 8 <= N) {
+                    put8(out + (int64_t)tk * N + c, acc[n][m], acc[n + 1][m]);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 8; ++e)
@@ -472,9 +471,9 @@ struct Fp8Plan {
 // The variant of the least estimated time: the launch, the rounds of work-groups over 256 CUs (but
 // no less than the weights' bytes take), and the partial sums of a split K. Its constants are a fit
 // to every tile with 1, 2 and 4 chunks and the rows, at 1 to 4096 tokens, 256 to 28672 rows and 512
-// to 14336 columns (11000 times, off by 11% in the mean); the variants it takes are 1.5% slower than
-// the best of each size in the mean, where "the largest tile that fills the chip" lost 7%. Some of
-// them, in us:
+// to 14336 columns (11000 times, off by 11% in the mean); the variants it takes are 1.5% slower
+// than the best of each size in the mean, where "the largest tile that fills the chip" lost 7%.
+// Some of them, in us:
 //   13 tokens, 11008 x 4096    64 x 64 9.9, in two chunks 13.0, rows 14.8
 //   13 tokens, 4096 x 14336    64 x 64 23.8, in two chunks 16.0, in four 14.3
 //    5 tokens, 14336 x 14336   64 x 64 39, 256 x 256 in four chunks 64
