@@ -471,7 +471,7 @@ struct Fp8Plan {
 // The variant of the least estimated time: the launch, the rounds of work-groups over 256 CUs (but
 // no less than the weights' bytes take), and the partial sums of a split K. Its constants are a fit
 // to every tile with 1, 2 and 4 chunks and the rows, at 1 to 4096 tokens, 256 to 28672 rows and 512
-// to 14336 columns (11000 times, off by 11% in the mean); the variants it takes are 1.5% slower
+// to 14336 columns (14100 times, off by 11% in the mean); the variants it takes are 1.5% slower
 // than the best of each size in the mean, where "the largest tile that fills the chip" lost 7%.
 // Some of them, in us:
 //   13 tokens, 11008 x 4096    64 x 64 9.9, in two chunks 13.0, rows 14.8
