@@ -522,8 +522,9 @@ int si_moe_route(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* 
  *
  * Accumulation is float32; h = SiLU(g) * u is float32 and enters the down product as float32
  * (float32 weights), as bf16 parts of 16 significant bits in all (24 with a float32 y), or with
- * half weights as a half pair of 22 bits for |h| < 2^24. Each chosen expert's weights are read
- * once per 16 to 128 of its tokens. An infinite down weight of 16 bits may give NaN where the
+ * half weights as a half pair, scaled by the largest finite |h| of the (token, rank): 22 bits, or
+ * an error of 2^-50 of that largest where it is more. Each chosen expert's weights are read once
+ * per 16 to 128 of its tokens. An infinite down weight of 16 bits may give NaN where the
  * formula gives an infinity (it meets the lower parts of h). Requires 0 <= T <= 512,
  * 1 <= k <= 32, T * k <= 8192, 1 <= E <= 65535; d and I multiples of 4 (float32), 8 (16-bit) or
  * 16 (SI_E4M3), d, I <= 65536; one expert's gate and up rows, x as float32, and the parts of h

@@ -7,7 +7,7 @@
 // and every product runs on MFMAs whose token operand is mostly padding (16 tokens a tile), which
 // is free below the weights' rate. Three kernels: gate/up with SiLU(g) * u, down, weighted sum; two
 // for one token, the router's choice included; two others for many tokens an expert, whose waves
-// share the tokens' operand.
+// share the tokens' operand. Half weights take one more between gate/up and down (moe_h_parts).
 //
 // A pair is an entry p = t * k + r of ids. A work-group takes one expert and a tile of weight
 // rows, finds the expert's pairs by reading ids itself (no list kernel, no launch that waits for
@@ -21,8 +21,8 @@
 // Element types: float32, bf16, half, or e4m3 codes with a float32 scale for each 128 x 128
 // weights. Codes become the 16-bit type of x (exactly); a scale block's products are summed in
 // float32 and then scaled into the total. h enters the down product in parts of 16 bits: bf16
-// hi + lo (16 bits), hi + mid + lo (24 bits) when y is float32, and half hi + lo (22 bits); the
-// extra MFMAs are free for the same reason.
+// hi + lo (16 bits), hi + mid + lo (24 bits) when y is float32, and half hi + lo (22 bits) of h
+// times a power of two by the pair's largest |h|; the extra MFMAs are free for the same reason.
 #include <type_traits>
 
 #include "common.h"
@@ -302,12 +302,44 @@ struct HType {
 };
 template <>
 struct HType<f16_t, true> {
-    typedef bf16_t type;  // codes are exact in either type, and bf16 parts have no range limit
+    typedef bf16_t type;  // codes are exact in either type, and bf16 parts need no scale
 };
 
-// h of half weights is kept as h / 256, so that it may reach 2^24 instead of 65504; the parts
-// below the first carry a factor 2^11 each, which keeps them from being subnormal
-constexpr float kHalfDown = 1.0f / 256.0f, kHalfUp = 256.0f;
+// What gate and up write: the parts of h, or, of half weights, h itself. A half holds 11 bits from
+// 2^-14 to 2^16 alone, so their parts are those of h * 2^e, by the largest finite |h| of the pair
+// (half_scale): hi, and what hi leaves out times 2^11. That is 22 bits of each value down to 2^-27
+// of the largest, and below that a step of 2^-49 of it, whatever the size of h. The largest is known
+// when the pair's last neuron is, so the parts are a kernel of their own (moe_h_parts).
+// (Parts of h / 256, without the maximum, lost bits below 2^-6 and everything below 2^-28.)
+template <typename XT, bool FP8>
+struct GateOut {
+    typedef typename HType<XT, FP8>::type type;
+};
+template <>
+struct GateOut<f16_t, false> {
+    typedef float type;
+};
+
+constexpr float kLoUp = 2048.0f, kLoDown = 1.0f / 2048.0f;
+
+// bits of |v|, 0 for an infinity or a NaN
+__device__ __forceinline__ uint32_t finite_bits(float v) {
+    const uint32_t u = __float_as_uint(v) & 0x7fffffffu;
+    return u < 0x7f800000u ? u : 0u;
+}
+// up = 2^e that takes the largest |h| (by its bits) to [2^14, 2^15), and down = 2^-e; e <= 126
+// keeps both normal
+__device__ __forceinline__ void half_scale(uint32_t top, float& up, float& down) {
+    const int e = min(126, 141 - (int)(top >> 23));
+    up = __uint_as_float((uint32_t)(127 + e) << 23);
+    down = __uint_as_float((uint32_t)(127 - e) << 23);
+}
+// the two parts of v = h * 2^e; an infinite or NaN h stays in the first alone
+__device__ __forceinline__ void half_parts(float v, f16_t& hi, f16_t& lo) {
+    hi = (f16_t)v;
+    const float r = (v - (float)hi) * kLoUp;
+    lo = (f16_t)(fabsf(r) < HUGE_VALF ? r : 0.0f);
+}
 
 __device__ __forceinline__ void put_h(float h, int64_t at, int64_t plane, int parts, float* o) {
     o[at] = h;
@@ -324,14 +356,15 @@ __device__ __forceinline__ void put_h(float h, int64_t at, int64_t plane, int pa
         if (!(fabsf(h) < HUGE_VALF)) h = 0.0f;
     }
 }
-__device__ __forceinline__ void put_h(float h, int64_t at, int64_t plane, int parts, f16_t* o) {
-    h *= kHalfDown;
-    for (int p = 0; p < parts; ++p) {
-        const f16_t b = (f16_t)h;
-        o[p * plane + at] = b;
-        h = (h - (float)b) * 2048.0f;
-        if (!(fabsf(h) < HUGE_VALF)) h = 0.0f;
-    }
+// h of four neurons, at a multiple of 4 (rows of h hold a multiple of 4 too)
+__device__ __forceinline__ void put_h4(const f32x4_t& h, int64_t at, int64_t plane, int parts,
+                                       float* o) {
+    *reinterpret_cast<f32x4_t*>(o + at) = h;
+}
+__device__ __forceinline__ void put_h4(const f32x4_t& h, int64_t at, int64_t plane, int parts,
+                                       bf16_t* o) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) put_h(h[e], at + e, plane, parts, o);
 }
 
 // LDS of a wave: its ring, which the sums of the waves reuse. Passes of 16, 32 and 64 tokens keep
@@ -383,7 +416,7 @@ __device__ __forceinline__ void join_waves(const f32x4_t* acc, f32x4_t* red, int
 template <typename XT, bool FP8, int RING, int WK, int NR, int NT>
 __device__ __forceinline__ void gate_up_pass(
     const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
-    const uint16_t* list, int m, typename HType<XT, FP8>::type* H, int64_t plane, int parts, int wk,
+    const uint16_t* list, int m, typename GateOut<XT, FP8>::type* H, int64_t plane, int parts, int wk,
     char* ring, f32x4_t* red) {
     constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
     constexpr int RT = 2 * NR;  // tile 2 q: gate rows of neurons 16 q .., 2 q + 1: their up rows
@@ -429,11 +462,11 @@ __device__ __forceinline__ void gate_up_pass(
         const int nr = q / NT, n = q - nr * NT;
         if (16 * n + row < m) {
             const int64_t pair = list[16 * n + row];
+            const int j = n0 + 16 * nr + 4 * g;
+            f32x4_t h;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = n0 + 16 * nr + 4 * g + e;
-                if (j < I) put_h(silu_f32(sg[e]) * su[e], pair * I + j, plane, parts, H);
-            }
+            for (int e = 0; e < 4; ++e) h[e] = silu_f32(sg[e]) * su[e];
+            if (j < I) put_h4(h, pair * I + j, plane, parts, H);
         }
     };
     constexpr int NQ = NR * NT;
@@ -471,7 +504,7 @@ template <typename XT, bool FP8, int RING, int WK, int NR>
 __global__ __launch_bounds__(WK * 64) void moe_gate_up(
     const XT* __restrict__ x, int64_t T, int d, const int32_t* __restrict__ ids, int npairs, int k,
     const uint8_t* __restrict__ gate_up, const float* __restrict__ scales, int E, int I,
-    int by_pair, typename HType<XT, FP8>::type* __restrict__ H, int parts) {
+    int by_pair, typename GateOut<XT, FP8>::type* __restrict__ H, int parts) {
     extern __shared__ uint16_t list[];
     constexpr int MT = max_tiles<RING, FP8, 2 * NR, 1>();
     __shared__ __align__(1024) char rings[WK * RING];
@@ -504,22 +537,62 @@ __global__ __launch_bounds__(WK * 64) void moe_gate_up(
     }
 }
 
+// ---- parts of h, half weights ----------------------------------------------------------------
+// One work-group a pair: its largest finite |h|, then the parts of h * 2^e into two planes, and
+// 2^-e into hs. The row stays in registers between the two, V vectors of each of TH threads. It
+// costs its launch, 2.2 us of a layer's 25.4 for one token, and 4 bytes written, read and written a
+// value: 48 to 96 tokens over 8 experts of 14336 x 4096, from 1% less to 3% more than parts without
+// a scale. (Done by each work-group of moe_down_one in LDS, 2.3 us for one token.)
+template <int TH, int V>
+__global__ __launch_bounds__(TH) void moe_h_parts(const float* __restrict__ h,
+                                                  const int32_t* __restrict__ ids, int E, int I,
+                                                  int64_t plane, f16_t* __restrict__ H,
+                                                  float* __restrict__ hs) {
+    __shared__ uint32_t red[TH / kWave];
+    const int64_t pair = blockIdx.x;
+    if ((unsigned)ids[pair] >= (unsigned)E) return;  // no expert: no h was written
+    const f32x4_t* row = reinterpret_cast<const f32x4_t*>(h + pair * I);
+    const int n = I / 4;  // I is a multiple of 8
+    f32x4_t v[V];
+    uint32_t m = 0u;
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+        const int i = threadIdx.x + u * TH;
+        v[u] = i < n ? row[i] : f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
+    }
+#pragma unroll
+    for (int u = 0; u < V; ++u)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) m = max(m, finite_bits(v[u][e]));
+#pragma unroll
+    for (int q = 1; q < kWave; q <<= 1) m = max(m, (uint32_t)__shfl_xor((int)m, q, kWave));
+    if ((threadIdx.x & (kWave - 1)) == 0) red[threadIdx.x / kWave] = m;
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < TH / kWave; ++q) m = max(m, red[q]);
+    float up, down;
+    half_scale(m, up, down);
+    f16_t* const o = H + pair * I;
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+        const int i = threadIdx.x + u * TH;
+        if (i < n) {
+            f16_t p[2][4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) half_parts(v[u][e] * up, p[0][e], p[1][e]);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) __builtin_memcpy(o + q * plane + 4 * i, p[q], 8);
+        }
+    }
+    if (threadIdx.x == 0) hs[pair] = down;
+}
+
 // ---- down -----------------------------------------------------------------------------------
 // Work-group: WR groups of 16 RT rows of one expert's down matrix (columns of y), K split over WK
 // waves -> z[pair][d] float32.
 
-// factor of part p of h in the sum (half: see kHalfDown)
-template <typename HT>
-__device__ __forceinline__ float part_factor(int p) {
-    return 1.0f;
-}
-template <>
-__device__ __forceinline__ float part_factor<f16_t>(int p) {
-    return p == 0 ? kHalfUp : kHalfUp / 2048.0f;
-}
-
-// acc[0] = the sum of the parts' totals
-template <typename HT, int SUMS, int RT, int NT>
+// acc[0] = the sum of the parts' totals (half: the lower part counts 2^-11)
+template <int SUMS, int RT, int NT>
 __device__ __forceinline__ void join_parts(f32x4_t (&acc)[SUMS][RT][NT]) {
     if constexpr (SUMS > 1) {
         static_assert(SUMS == 2, "hi and lo");
@@ -529,15 +602,27 @@ __device__ __forceinline__ void join_parts(f32x4_t (&acc)[SUMS][RT][NT]) {
             for (int n = 0; n < NT; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    acc[0][r][n][e] = fmaf(part_factor<HT>(0), acc[0][r][n][e],
-                                           part_factor<HT>(1) * acc[1][r][n][e]);
+                    acc[0][r][n][e] = fmaf(kLoDown, acc[1][r][n][e], acc[0][r][n][e]);
     }
+}
+
+// four columns of z of a pair, whose h of half weights was taken times 1 / hs[pair]
+template <typename HT>
+__device__ __forceinline__ void put_z(float* z, int64_t pair, int d, int c, const float* hs,
+                                      f32x4_t s) {
+    if constexpr (std::is_same<HT, f16_t>::value) {
+        const float f = hs[pair];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[e] *= f;
+    }
+    *reinterpret_cast<f32x4_t*>(z + pair * d + c) = s;
 }
 
 template <typename HT, bool FP8, int PARTS, int RING, int WK, int RT, int NT>
 __device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int d, const uint8_t* dn,
                                           const float* dns, int I, int c0, const uint16_t* list,
-                                          int m, float* z, int wk, char* ring, f32x4_t* red) {
+                                          int m, const float* hs, float* z, int wk, char* ring,
+                                          f32x4_t* red) {
     constexpr int WB = FP8 ? 1 : (int)sizeof(HT);
     const int lane = threadIdx.x & 63;
     const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
@@ -577,13 +662,13 @@ __device__ __forceinline__ void down_pass(const HT* H, int64_t plane, int d, con
 #pragma unroll
             for (int n = 0; n < NT; ++n) acc[q][r][n] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
     lines<HT, FP8, RT, NT, PARTS, SUMS, D>(acc, wr, woff, rb, hr, xoff, hb, pl, sc, l0, l1, ring);
-    join_parts<HT>(acc);
+    join_parts(acc);
     join_waves<WK, RT * NT>(&acc[0][0][0], red, wk, lane, [&](int q, const f32x4_t& s) {
         const int r = q / NT, n = q - r * NT;
         const int c = c0 + 16 * r + 4 * g;
         // d is a multiple of 4: a lane's four columns are all in or all out
         if (16 * n + row < m && c < d)
-            *reinterpret_cast<f32x4_t*>(z + (int64_t)list[16 * n + row] * d + c) = s;
+            put_z<HT>(z, list[16 * n + row], d, c, hs, s);
     });
 }
 
@@ -591,7 +676,7 @@ template <typename HT, bool FP8, int PARTS, int RING, int WK, int WR, int RT>
 __global__ __launch_bounds__(WK * WR * 64) void moe_down(
     const HT* __restrict__ H, int d, const int32_t* __restrict__ ids, int npairs,
     const uint8_t* __restrict__ down, const float* __restrict__ scales, int E, int I, int by_pair,
-    float* __restrict__ z) {
+    const float* __restrict__ hs, float* __restrict__ z) {
     extern __shared__ uint16_t list[];
     constexpr int W = WK * WR;
     constexpr int MT = max_tiles<RING, FP8, RT, PARTS>();
@@ -613,7 +698,7 @@ __global__ __launch_bounds__(WK * WR * 64) void moe_down(
         const int mc = min(m - c, 16 * MT);
         auto pass = [&](auto tiles) {
             down_pass<HT, FP8, PARTS, RING, WK, RT, decltype(tiles)::value>(
-                H, plane, d, dn, ds, I, c0, list + c, mc, z, wk, ring, red);
+                H, plane, d, dn, ds, I, c0, list + c, mc, hs, z, wk, ring, red);
         };
         if (mc <= 16)
             pass(std::integral_constant<int, 1>());
@@ -735,7 +820,7 @@ __device__ __forceinline__ void wide_passes(int m, F pass) {
 template <typename XT, bool FP8, int NR, int NT, int S>
 __device__ __forceinline__ void gate_up_wide_pass(
     const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
-    const uint16_t* list, int m, typename HType<XT, FP8>::type* H, int64_t plane, int parts,
+    const uint16_t* list, int m, typename GateOut<XT, FP8>::type* H, int64_t plane, int parts,
     char* lds) {
     constexpr int RT = 2 * NR;
     const int lane = threadIdx.x & 63;
@@ -768,13 +853,12 @@ __device__ __forceinline__ void gate_up_wide_pass(
         const int nr = q / NT, n = q - nr * NT;
         if (16 * n + row < m) {
             const int64_t pair = list[16 * n + row];
+            const int j = n0 + 16 * nr + 4 * g;
+            f32x4_t h;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int j = n0 + 16 * nr + 4 * g + e;
-                if (j < I)
-                    put_h(silu_f32(acc[0][2 * nr][n][e]) * acc[0][2 * nr + 1][n][e], pair * I + j,
-                          plane, parts, H);
-            }
+            for (int e = 0; e < 4; ++e)
+                h[e] = silu_f32(acc[0][2 * nr][n][e]) * acc[0][2 * nr + 1][n][e];
+            if (j < I) put_h4(h, pair * I + j, plane, parts, H);
         }
     }
 }
@@ -783,7 +867,7 @@ template <typename XT, bool FP8, int NR>
 __global__ __launch_bounds__(kWide * 64) void moe_gate_up_wide(
     const XT* __restrict__ x, int64_t T, int d, const int32_t* __restrict__ ids, int npairs, int k,
     const uint8_t* __restrict__ gate_up, const float* __restrict__ scales, int E, int I,
-    int by_pair, typename HType<XT, FP8>::type* __restrict__ H, int parts) {
+    int by_pair, typename GateOut<XT, FP8>::type* __restrict__ H, int parts) {
     extern __shared__ uint16_t list[];
     constexpr int NTM = NR == 1 ? 4 : wide_tiles<FP8, 1>(), S = kWideStages;
     __shared__ __align__(1024) char lds[S * wide_stage<FP8, 2 * NR, NTM, 1, kWide>() * 1024];
@@ -809,7 +893,8 @@ __global__ __launch_bounds__(kWide * 64) void moe_gate_up_wide(
 template <typename HT, bool FP8, int PARTS, int NT, int S>
 __device__ __forceinline__ void down_wide_pass(const HT* H, int64_t plane, int d, const uint8_t* dn,
                                                const float* dns, int I, int c0,
-                                               const uint16_t* list, int m, float* z, char* lds) {
+                                               const uint16_t* list, int m, const float* hs,
+                                               float* z, char* lds) {
     constexpr int RT = 2, SUMS = std::is_same<HT, f16_t>::value ? PARTS : 1;
     const int lane = threadIdx.x & 63;
     const int row = lane & 15, g = lane >> 4, lr = lane >> 3;
@@ -838,7 +923,7 @@ __device__ __forceinline__ void down_wide_pass(const HT* H, int64_t plane, int d
         acc, make_rsrc(dn, (int64_t)d * rb), woff, rb,
         make_rsrc(H, (int64_t)PARTS * plane * sizeof(HT)), list, m, 1, I * (int)sizeof(HT),
         (int)(plane * sizeof(HT)), sc, nl, lds);
-    join_parts<HT>(acc);
+    join_parts(acc);
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int c = c0 + 16 * r + 4 * g;
@@ -846,7 +931,7 @@ __device__ __forceinline__ void down_wide_pass(const HT* H, int64_t plane, int d
         for (int n = 0; n < NT; ++n) {
             // d is a multiple of 4: a lane's four columns are all in or all out
             if (16 * n + row < m && c < d)
-                *reinterpret_cast<f32x4_t*>(z + (int64_t)list[16 * n + row] * d + c) = acc[0][r][n];
+                put_z<HT>(z, list[16 * n + row], d, c, hs, acc[0][r][n]);
         }
     }
 }
@@ -855,7 +940,7 @@ template <typename HT, bool FP8, int PARTS>
 __global__ __launch_bounds__(kWide * 64) void moe_down_wide(
     const HT* __restrict__ H, int d, const int32_t* __restrict__ ids, int npairs,
     const uint8_t* __restrict__ down, const float* __restrict__ scales, int E, int I, int by_pair,
-    float* __restrict__ z) {
+    const float* __restrict__ hs, float* __restrict__ z) {
     extern __shared__ uint16_t list[];
     constexpr int NTM = wide_tiles<FP8, PARTS>(), S = kWideStages;
     __shared__ __align__(1024) char lds[S * wide_stage<FP8, 2, NTM, PARTS, kWide>() * 1024];
@@ -870,7 +955,7 @@ __global__ __launch_bounds__(kWide * 64) void moe_down_wide(
     const int64_t plane = (int64_t)npairs * I;
     wide_passes<NTM>(m, [&](auto tiles, int c, int mc) {
         down_wide_pass<HT, FP8, PARTS, decltype(tiles)::value, S>(H, plane, d, dn, ds, I, c0,
-                                                                  list + c, mc, z, lds);
+                                                                  list + c, mc, hs, z, lds);
     });
 }
 
@@ -1020,7 +1105,7 @@ template <typename XT, bool FP8, bool CHOOSE>
 __global__ __launch_bounds__(256) void moe_gate_up_one(
     const XT* __restrict__ x, int d, Choice choice, int32_t* __restrict__ ids,
     float* __restrict__ weights, int k, const uint8_t* __restrict__ gate_up,
-    const float* __restrict__ scales, int E, int I, typename HType<XT, FP8>::type* __restrict__ H,
+    const float* __restrict__ scales, int E, int I, typename GateOut<XT, FP8>::type* __restrict__ H,
     int parts) {
     constexpr int W = 4, D = 4, RT = 2;
     __shared__ __align__(1024) char rings[W * D * 2 * RT * 1024];
@@ -1096,9 +1181,10 @@ constexpr int kOneWaves = 8;
 
 template <typename HT, bool FP8, int PARTS, typename YT>
 __global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
-    const HT* __restrict__ H, int d, const int32_t* __restrict__ ids,
-    const float* __restrict__ weights, int k, int kc, const uint8_t* __restrict__ down,
-    const float* __restrict__ scales, int E, int I, YT* __restrict__ y) {
+    const HT* __restrict__ H, const float* __restrict__ hscale, int d,
+    const int32_t* __restrict__ ids, const float* __restrict__ weights, int k, int kc,
+    const uint8_t* __restrict__ down, const float* __restrict__ scales, int E, int I,
+    YT* __restrict__ y) {
     constexpr int D = 6;
     __shared__ __align__(1024) char rings[kOneWaves * D * 2 * 1024];
     extern __shared__ __align__(1024) char hs[];
@@ -1139,11 +1225,16 @@ __global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
                                         });
         if (some) {
             const float f = weights[r];
+            if constexpr (std::is_same<HT, f16_t>::value) {
+                const float back = hscale[r];
 #pragma unroll
-            for (int p = PARTS - 1; p >= 0; --p) {
-                const float fp = std::is_same<HT, f16_t>::value ? f * part_factor<HT>(p) : f;
+                for (int i = 0; i < 4; ++i)
+                    tot[i] = fmaf(f, fmaf(kLoDown, acc[0][1][i], acc[0][0][i]) * back, tot[i]);
+            } else {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tot[i] = fmaf(fp, acc[0][p][i], tot[i]);
+                for (int p = PARTS - 1; p >= 0; --p)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) tot[i] = fmaf(f, acc[0][p][i], tot[i]);
             }
         }
     }
@@ -1172,7 +1263,7 @@ __global__ __launch_bounds__(kOneWaves * 64) void moe_down_one(
 struct Plan {
     int64_t pairs;
     int parts, hbytes;  // parts of h and bytes of an element of one
-    size_t off_z, total;
+    size_t off_z, off_h, off_s, total;  // (half weights: h in float32, and the pairs' scales)
 };
 Plan moe_plan(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt, int ydt) {
     Plan p;
@@ -1185,7 +1276,10 @@ Plan moe_plan(int64_t T, int64_t k, int64_t d, int64_t I, int xdt, int wdt, int 
         p.parts = (xdt == 2 && wdt == 2) ? 2 : (ydt == 0 ? 3 : 2);
     }
     p.off_z = ((size_t)p.pairs * I * p.parts * p.hbytes + 255) / 256 * 256;
-    p.total = p.off_z + (size_t)p.pairs * d * sizeof(float);
+    p.off_h = p.off_z + ((size_t)p.pairs * d * sizeof(float) + 255) / 256 * 256;
+    const bool half = xdt == 2 && wdt == 2;
+    p.off_s = p.off_h + (half ? ((size_t)p.pairs * I * sizeof(float) + 255) / 256 * 256 : 0);
+    p.total = p.off_s + (half ? (size_t)p.pairs * sizeof(float) : 0);
     return p;
 }
 
@@ -1240,8 +1334,13 @@ constexpr int64_t kWidePairs = 48;
 template <typename XT, bool FP8, int PARTS>
 void experts(const Args& a) {
     typedef typename HType<XT, FP8>::type HT;
+    typedef typename GateOut<XT, FP8>::type GT;
+    constexpr bool HALF = std::is_same<HT, f16_t>::value;
     HT* H = static_cast<HT*>(a.ws);
     float* z = reinterpret_cast<float*>(static_cast<char*>(a.ws) + a.p.off_z);
+    // what gate and up write
+    GT* G = reinterpret_cast<GT*>(static_cast<char*>(a.ws) + (HALF ? a.p.off_h : 0));
+    float* hs = reinterpret_cast<float*>(static_cast<char*>(a.ws) + a.p.off_s);
     const int np = (int)a.p.pairs;
     // fewer pairs than experts: a slot a pair, so that no work-group is without an expert but
     // those of repeated ones; else a slot an expert
@@ -1261,16 +1360,16 @@ void experts(const Args& a) {
         if (a.choice)
             moe_gate_up_one<XT, FP8, true><<<grid, 256, (size_t)xlds, a.s>>>(
                 x, (int)a.d, *a.choice, a.ids, a.w, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I,
-                H, a.p.parts);
+                G, a.p.parts);
         else
             moe_gate_up_one<XT, FP8, false><<<grid, 256, (size_t)xlds, a.s>>>(
                 x, (int)a.d, Choice{}, a.ids, a.w, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I,
-                H, a.p.parts);
+                G, a.p.parts);
     } else {
         auto gate = [&](auto kernel, int rows, int threads) {
             kernel<<<dim3((unsigned)((a.I + rows - 1) / rows), slots), threads, lds, a.s>>>(
                 x, a.T, (int)a.d, a.ids, np, (int)a.k, a.gate_up, a.gus, (int)a.E, (int)a.I,
-                by_pair, H, a.p.parts);
+                by_pair, G, a.p.parts);
         };
         if (many) {
             if constexpr (FP8) {
@@ -1287,9 +1386,21 @@ void experts(const Args& a) {
             gate(moe_gate_up<XT, FP8, 24 * 1024, 2, 1>, 16, 128);
         }
     }
+    if constexpr (HALF) {
+        auto parts = [&](auto kernel, int threads) {
+            kernel<<<dim3((unsigned)np), threads, 0, a.s>>>(G, a.ids, (int)a.E, (int)a.I,
+                                                            (int64_t)np * a.I, H, hs);
+        };
+        // (rows up to 65536 values; short ones by the large work-group: 128 tokens, 6 of 64 experts
+        // of 1024 x 1024 132 us instead of 124, one token, 8 of 768 x 2048 27.3 instead of 25.4)
+        if (a.I <= 4096)
+            parts(moe_h_parts<256, 4>, 256);
+        else
+            parts(moe_h_parts<1024, 16>, 1024);
+    }
     // f(y) with y's type: bf16 parts number 3 for a float32 y and 2 for one of 16 bits
     auto to_y = [&](auto f) {
-        constexpr bool kF32 = PARTS != 2 || std::is_same<HT, f16_t>::value;
+        constexpr bool kF32 = PARTS != 2 || HALF;
         if constexpr (PARTS == 2) {
             if (!kF32 || a.ydt != 0) return f(static_cast<XT*>(a.y));
         }
@@ -1303,14 +1414,14 @@ void experts(const Args& a) {
         auto one = [&](auto* y) {
             typedef typename std::remove_pointer<decltype(y)>::type YT;
             moe_down_one<HT, FP8, PARTS, YT><<<grid, kOneWaves * 64, (size_t)hlds, a.s>>>(
-                H, (int)a.d, a.ids, a.w, (int)a.k, kc, a.down, a.dns, (int)a.E, (int)a.I, y);
+                H, hs, (int)a.d, a.ids, a.w, (int)a.k, kc, a.down, a.dns, (int)a.E, (int)a.I, y);
         };
         to_y(one);
         return;
     }
     auto down = [&](auto kernel, int rows, int threads) {
         kernel<<<dim3((unsigned)((a.d + rows - 1) / rows), slots), threads, lds, a.s>>>(
-            H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, z);
+            H, (int)a.d, a.ids, np, a.down, a.dns, (int)a.E, (int)a.I, by_pair, hs, z);
     };
     if (many) {
         if constexpr (kMany) down(moe_down_wide<HT, FP8, PARTS>, 32 * kWide, kWide * 64);
