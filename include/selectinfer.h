@@ -430,8 +430,8 @@ int si_load_selected(const void* w_gate, const void* w_up, const void* w_down, i
  *   a = max(max |x| of the block, 2^-60),  scale = a / 448,  code = e4m3(x * (448 / a))
  *
  * in float32, codes rounded to nearest even. A block that holds a NaN or an infinity gets scale
- * NaN and NaN codes. Requires G, R >= 0, C >= 1, C % 16 == 0, 16-byte aligned x and codes, fewer
- * than 2^28 (block_rows = 1) or 2^23 blocks. G * R = 0 enqueues nothing. Asynchronous,
+ * NaN and NaN codes. Requires G, R >= 0, C >= 1, C % 16 == 0, 16-byte aligned x and codes, at most
+ * 2^28 - 16 (block_rows = 1) or 2^23 - 1 blocks. G * R = 0 enqueues nothing. Asynchronous,
  * stream-ordered.
  */
 int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C, int block_rows,

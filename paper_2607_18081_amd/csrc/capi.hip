@@ -493,10 +493,12 @@ int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C
     if (!valid_dtype(xdt)) return SI_ERR_UNSUPPORTED;
     if (C % 16 != 0) return SI_ERR_UNSUPPORTED;
     if (G == 0 || R == 0) return SI_OK;
-    // no product below leaves 64 bits, and a launch holds fewer than 2^32 threads
+    // no product below leaves 64 bits, and a launch holds fewer than 2^32 threads (256 for each 16
+    // blocks of 1 x 128, 512 for one of 128 x 128)
     constexpr int64_t top = (int64_t)1 << 31;
     if (G > top || R > top || C > top || G > ((int64_t)1 << 36) / R ||
-        si::quant_blocks(G, R, C, block_rows) >= (int64_t)1 << (block_rows == 1 ? 28 : 23))
+        si::quant_blocks(G, R, C, block_rows) >
+            (block_rows == 1 ? ((int64_t)1 << 28) - 16 : ((int64_t)1 << 23) - 1))
         return SI_ERR_UNSUPPORTED;
     if (!x || !codes || !scales || !aligned16(x) || !aligned16(codes)) return SI_ERR_INVALID;
     return from_hip(si::launch_quant(x, xdt, G, R, C, block_rows, codes, scales,
