@@ -20,9 +20,6 @@ namespace si {
 namespace {
 
 // ---- logits ------------------------------------------------------------------------------
-// One work-group of 4 waves a tile of 16 experts x 16 tokens and a K chunk; the waves take K
-// steps in turn. The experts' rows are the MFMA's M operand, tokens its N operand.
-
 // One K step: 16 bytes of a weight row a lane (four lanes a row: 32 values of 16-bit data, 16 of
 // float32), and the same columns of a token.
 template <typename XT, typename WT>

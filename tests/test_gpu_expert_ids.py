@@ -51,3 +51,40 @@ def test_one_expert_at_every_rank(T, E, dt, wkind):
     args = [torch.from_numpy(v).to(DEV) for v in (ids, weights)]
     y = si.moe_ffn(x, *args, dev[0], dev[1], gate_up_scales=dev[2], down_scales=dev[3])
     _check_layer(y, x, args[0], args[1], gu, dn, dt, wkind)
+
+
+@pytest.mark.parametrize("dt,wkind", [("bf16", "same"), ("f16", "same"), ("f32", "same"),
+                                      ("bf16", "fp8"), ("f16", "fp8")])
+@pytest.mark.parametrize("T,E", [(1, 8), (1, 300), (3, 8), (40, 2)])
+def test_padding_comes_and_goes(T, E, dt, wkind):
+    """A captured layer whose n_valid goes from all to none and back between replays, with eager
+    work between; the rows behind are NaN in x, and 0 in y. The choice is made in a kernel of its
+    own, or (one token, few experts) in the experts' first one."""
+    say(f"padding comes and goes T={T} E={E} {dt} {wkind}")
+    d, inter, k = 64, 80, 2
+    dev, gu, dn = _experts(E, d, inter, dt, wkind, T + E)
+    g = torch.Generator().manual_seed(E)
+    x = torch.randn(T, d, generator=g).to(DT[dt]).to(DEV)
+    w = (torch.randn(E, d, generator=g) / 8).to(DT[dt]).to(DEV)
+    kw = dict(gate_up_scales=dev[2], down_scales=dev[3])
+    whole, ids_w, weights_w = si.moe_layer(x, w, dev[0], dev[1], k, **kw)
+    _check_layer(whole, x, ids_w, weights_w, gu, dn, dt, wkind)
+    held = x.clone()
+    n = torch.tensor([T], dtype=torch.int32, device=DEV)
+    y = torch.empty(T, d, device=DEV)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        _, ids, weights = si.moe_layer(held, w, dev[0], dev[1], k, n_valid=n, y=y, **kw)
+    for valid in (T, 0, T, T - 1, 0, 0, T):
+        held.copy_(x)
+        held[valid:] = float("nan")
+        n.fill_(valid)
+        y.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y[:valid], whole[:valid]) and torch.all(y[valid:] == 0), valid
+        assert torch.equal(ids[:valid], ids_w[:valid]) and torch.all(ids[valid:] == -1)
+        assert torch.equal(weights[:valid], weights_w[:valid]) and torch.all(weights[valid:] == 0)
+        again, _, _ = si.moe_layer(held, w, dev[0], dev[1], k, n_valid=n, **kw)
+        assert torch.equal(again, y)
