@@ -525,7 +525,8 @@ int si_moe_route(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* 
  *   y        [T][d] out    ydt: SI_F32 or x's type, rounded once
  *   ws                     workspace of si_moe_ffn_workspace(...) bytes
  *
- * Accumulation is float32; h = SiLU(g) * u is float32 and enters the down product as float32
+ * Accumulation is float32; h = SiLU(g) * u is float32 (SiLU by the hardware's exponential and
+ * reciprocal, within (|g| + 4) 2^-23 of its value, and 0 below g = -87) and enters the down product as float32
  * (float32 weights), as bf16 parts of 16 significant bits in all (24 with a float32 y), or with
  * half weights as a half pair, scaled by the largest finite |h| of the (token, rank): 22 bits, or
  * an error of 2^-50 of that largest where it is more. Each chosen expert's weights are read once

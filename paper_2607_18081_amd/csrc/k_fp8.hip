@@ -176,8 +176,8 @@ __global__ __launch_bounds__(kRowWaves * 64) void fp8_rows(
 // 4096 tokens, 14336 x 4096: 230 us, 2.1 PFLOP/s, once the clocks have settled, some 150 launches
 // on; 249 in the first five, up to 315 after them. (With one scale a tensor the library's product
 // takes 164 settled, 200 before.) What bounds it: the loads of a step, 64 KB a CU from the XCD's L2.
-// In the first launches, where the kernel took 271 us: without the MFMAs 255, without memory behind
-// the loads 210, without the stores 226. In the order found, by such launches too:
+// By the first launches: without the MFMAs 255 us, without memory behind the loads 210, without the
+// stores 226. In the order found, by such launches too:
 // the compiler's own waits for the loads just issued (one array a stage, 402 -> 280 us; the loop
 // must also not be left in mid-round, or the accumulators live twice and spill), lines first read
 // one step before use (touched ahead, 295 -> 271), prologue and stores of each tile (loads run on
@@ -263,9 +263,9 @@ __global__ __launch_bounds__(WN * WM * 64) void fp8_tiles(
     // touches its share of the lines of a later step (one word a line, into LDS that nothing
     // reads), which then come from the XCD's L2. The word is the block's last: where K is no
     // multiple of 128, blocks begin and end inside lines, and the first line was touched a step
-    // before. It helps where few tiles share a line and costs where many do (settled clocks; 4096
-    // tokens, 14336 x 4112: 284 us by the blocks' first words, 266 by the last; 2079, 14146 x 8176:
-    // 267 and 290; 4096, 14336 x 8176: 520 and 523; K = 4096: 231 and 231).
+    // before. It is not better for every such K (settled clocks; 4096 tokens, 14336 x 4112: 284 us by
+    // the blocks' first words, 266 by the last; 2079, 14146 x 8176: 267 and 290; 4096, 14336 x 8176:
+    // 520 and 523; K = 4096: 231 and 231).
     const int sharew = min(8, ntm), sharex = max(1, 32 / sharew);
     const int rx = (BM + sharex - 1) / sharex, rw = (BN + sharew - 1) / sharew;
     constexpr int kLoads = LA + LB + (TOUCH ? 2 : 1);

@@ -470,34 +470,28 @@ __device__ __forceinline__ void gate_up_pass(
         }
     };
     constexpr int NQ = NR * NT;
-    if constexpr (WK == 1) {
+    __syncthreads();  // the rings are done with
 #pragma unroll
-        for (int q = 0; q < NQ; ++q)
-            finish(q, acc[2 * (q / NT)][q % NT], acc[2 * (q / NT) + 1][q % NT]);
-    } else {
-        __syncthreads();  // the rings are done with
+    for (int q = 0; q < NQ; ++q)
 #pragma unroll
-        for (int q = 0; q < NQ; ++q)
+        for (int r = 0; r < 2; ++r)
+            red[((wk * NQ + q) * 2 + r) * 64 + lane] = acc[2 * (q / NT) + r][q % NT];
+    __syncthreads();
+    for (int q = wk; q < NQ; q += WK) {
+        f32x4_t s[2];
 #pragma unroll
-            for (int r = 0; r < 2; ++r)
-                red[((wk * NQ + q) * 2 + r) * 64 + lane] = acc[2 * (q / NT) + r][q % NT];
-        __syncthreads();
-        for (int q = wk; q < NQ; q += WK) {
-            f32x4_t s[2];
+        for (int r = 0; r < 2; ++r) {
+            s[r] = red[(q * 2 + r) * 64 + lane];
 #pragma unroll
-            for (int r = 0; r < 2; ++r) {
-                s[r] = red[(q * 2 + r) * 64 + lane];
+            for (int w = 1; w < WK; ++w) {
+                const f32x4_t v = red[((w * NQ + q) * 2 + r) * 64 + lane];
 #pragma unroll
-                for (int w = 1; w < WK; ++w) {
-                    const f32x4_t v = red[((w * NQ + q) * 2 + r) * 64 + lane];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) s[r][e] += v[e];
-                }
+                for (int e = 0; e < 4; ++e) s[r][e] += v[e];
             }
-            finish(q, s[0], s[1]);
         }
-        __syncthreads();  // before the next pass's loads
+        finish(q, s[0], s[1]);
     }
+    __syncthreads();  // before the next pass's loads
 }
 
 template <typename XT, bool FP8, int RING, int WK, int NR>

@@ -144,3 +144,25 @@ def test_half_weights_workspace(T, E, k, d, inter, out):
     _check(y, _np(x), ids.cpu().numpy(), _np(weights), _np(gu), _np(dn))
     space.fill_(0)
     assert torch.equal(y, si.moe_ffn(x, ids, weights, gu, dn, out_dtype=out, workspace=space))
+
+
+def test_silu():
+    """SiLU(g) alone: unit rows make g and u = 1, and a float32 layer returns h. Error of the
+    exponential: a rounding of g log2(e) (|g| 2^-23 with the constant's own) and 2^-23; of the sum,
+    the reciprocal and the product: 2^-24, 2^-23 and 2^-24. Past 2^126 the reciprocal is 0."""
+    say("SiLU alone")
+    T, d, inter = 512, 4, 4
+    g = torch.linspace(-110.0, 110.0, T, dtype=torch.float64).float()
+    g[:8] = torch.tensor([0.0, -0.0, 1e-30, -1e-30, 1e30, 3e38, -1e30, -3e38])
+    x = torch.zeros(T, d)
+    x[:, 0], x[:, 1] = g, 1.0
+    gu, dn = torch.zeros(1, 2, inter, d), torch.zeros(1, d, inter)
+    gu[0, 0, :, 0], gu[0, 1, :, 1], dn[0, 2, 1] = 1.0, 1.0, 1.0
+    y = si.moe_ffn(x.to(DEV), torch.zeros(T, 1, dtype=torch.int32, device=DEV),
+                   torch.ones(T, 1, device=DEV), gu.to(DEV), dn.to(DEV))
+    v = g.double().numpy()
+    with np.errstate(over="ignore"):
+        want = v / (1.0 + np.exp(-v))
+    err = np.abs(_np(y[:, 2]) - want)
+    assert np.all(err <= (np.minimum(np.abs(v), 120.0) + 4.0) * 2.0 ** -23 * np.abs(want) + 1e-36)
+    assert torch.all(y[:, :2] == 0) and torch.all(y[:, 3] == 0)
