@@ -449,16 +449,18 @@ int si_quantize_fp8(const void* x, si_dtype xdt, int64_t G, int64_t R, int64_t C
  *   ws       workspace of si_matmul_fp8_workspace(M, N, K) bytes (NULL when that is 0)
  *
  * Blocks are added in float32; the two scales are multiplied first, in float32 (below 2^-126 their
- * product has fewer bits, past 2^128 it is infinite). The products of a block are summed in float32
- * for a float32 y. For a 16-bit y the 8-bit matrix instruction sums them: of each 8 consecutive
- * columns it cuts every product, towards zero, to a multiple of 2^-13 of the largest of their powers
- * of two (the two codes' exponents added, -6 for codes below 2^-6), so that each 8 columns are off by
- * less than 7 such steps. With random codes that is 1.5e-5 of y. It is a share of the products, not
- * of y: where large products of 8 columns cancel, or cancel against others, it may pass the rounding
- * of y (pairs of codes 448 that cancel: a half y off by 1.6e-3 instead of 2e-4). A caller whom that
- * touches takes a float32 y. A NaN code or scale makes the outputs it enters NaN. Requires M >= 0, N, K >= 1, K % 16 == 0, K <= 2^20, M, N <= 2^24,
- * M * N <= 2^40, 16-byte aligned x, w, y and ws. M = 0 enqueues nothing. Asynchronous,
- * stream-ordered.
+ * product has fewer bits, past 2^128 it is infinite). The products of a block are summed in
+ * float32 for a float32 y. For a 16-bit y the 8-bit matrix instruction sums them: of each 8
+ * consecutive columns it cuts every product, towards zero, to a multiple of 2^-13 of the largest
+ * of their powers of two (the two codes' exponents added, -6 for codes below 2^-6), so that each 8
+ * columns are off by less than 7 such steps. With random codes that is 1.5e-5 of y. It is a share
+ * of the products, not of y: where large products of 8 columns cancel, or cancel against others,
+ * it may pass the rounding of y (pairs of codes 448 that cancel: a half y off by 1.6e-3 instead of
+ * 2e-4). A caller whom that touches takes a float32 y.
+ *
+ * A NaN code or scale makes the outputs it enters NaN. Requires M >= 0, N, K >= 1, K % 16 == 0, K
+ * <= 2^20, M, N <= 2^24, M * N <= 2^40, 16-byte aligned x, w, y and ws. M = 0 enqueues nothing.
+ * Asynchronous, stream-ordered.
  *
  * si_matmul_fp8_plan: plan[0..1], weight rows and tokens of the tile that a call of these sizes
  * takes (0, 0: 16 rows with all tokens), plan[2], its K chunks (for tests and measurements).
@@ -526,16 +528,16 @@ int si_moe_route(const void* x, si_dtype xdt, int64_t T, int64_t d, const void* 
  *   ws                     workspace of si_moe_ffn_workspace(...) bytes
  *
  * Accumulation is float32; h = SiLU(g) * u is float32 (SiLU by the hardware's exponential and
- * reciprocal, within (|g| + 4) 2^-23 of its value, and 0 below g = -87) and enters the down product as float32
- * (float32 weights), as bf16 parts of 16 significant bits in all (24 with a float32 y), or with
- * half weights as a half pair, scaled by the largest finite |h| of the (token, rank): 22 bits, or
- * an error of 2^-50 of that largest where it is more. Each chosen expert's weights are read once
- * per 16 to 128 of its tokens. An infinite down weight of 16 bits may give NaN where the
- * formula gives an infinity (it meets the lower parts of h). Requires 0 <= T <= 512,
- * 1 <= k <= 32, T * k <= 8192, 1 <= E <= 65535; d and I multiples of 4 (float32), 8 (16-bit) or
- * 16 (SI_E4M3), d, I <= 65536; one expert's gate and up rows, x as float32, and the parts of h
- * (T * k * I values) each below 2 GiB, else SI_ERR_UNSUPPORTED; 16-byte aligned x, gate_up, down,
- * y and ws. Asynchronous, stream-ordered, deterministic.
+ * reciprocal, within (|g| + 4) 2^-23 of its value, and 0 below g = -87) and enters the down
+ * product as float32 (float32 weights), as bf16 parts of 16 significant bits in all (24 with a
+ * float32 y), or with half weights as a half pair, scaled by the largest finite |h| of the (token,
+ * rank): 22 bits, or an error of 2^-50 of that largest where it is more. Each chosen expert's
+ * weights are read once per 16 to 128 of its tokens. An infinite down weight of 16 bits may give
+ * NaN where the formula gives an infinity (it meets the lower parts of h). Requires 0 <= T <= 512,
+ * 1 <= k <= 32, T * k <= 8192, 1 <= E <= 65535; d and I multiples of 4 (float32), 8 (16-bit) or 16
+ * (SI_E4M3), d, I <= 65536; one expert's gate and up rows, x as float32, and the parts of h (of
+ * T * k * I values) each below 2 GiB, else SI_ERR_UNSUPPORTED; 16-byte aligned x, gate_up, down, y and
+ * ws. Asynchronous, stream-ordered, deterministic.
  */
 size_t si_moe_ffn_workspace(int64_t T, int64_t k, int64_t E, int64_t d, int64_t I, si_dtype xdt,
                             si_dtype wdt, si_dtype ydt);

@@ -416,8 +416,8 @@ __device__ __forceinline__ void join_waves(const f32x4_t* acc, f32x4_t* red, int
 template <typename XT, bool FP8, int RING, int WK, int NR, int NT>
 __device__ __forceinline__ void gate_up_pass(
     const XT* x, int64_t xbytes, int d, int k, const uint8_t* gu, const float* gus, int I, int n0,
-    const uint16_t* list, int m, typename GateOut<XT, FP8>::type* H, int64_t plane, int parts, int wk,
-    char* ring, f32x4_t* red) {
+    const uint16_t* list, int m, typename GateOut<XT, FP8>::type* H, int64_t plane, int parts,
+    int wk, char* ring, f32x4_t* red) {
     constexpr int WB = FP8 ? 1 : (int)sizeof(XT);
     constexpr int RT = 2 * NR;  // tile 2 q: gate rows of neurons 16 q .., 2 q + 1: their up rows
     constexpr int D = ring_depth<RING, FP8, RT, NT, 1>();
